@@ -332,6 +332,79 @@ const char* l2l_noalloc_last_error(void);
 int l2l_op_layernorm(l2l_ctx*, int dtype, int rows, int n, const void* x, const void* gamma,
                      const void* beta, float eps, void* y, float* mean, float* rstd);
 
+/* ---- single operations of fine-tuning ------------------------------------------------------------------------------
+   What the paper's GLUE runs (Sections 3.1 and 3.5) have around the encoder layer and the layer calls above leave out: sequences of
+   different lengths, dropout, and scores of single tokens.  All run on compute_stream, allocate nothing, keep nothing from
+   one call for the next and may be captured into a HIP graph; workspaces are the caller's, hold nothing between calls but what is said
+   here, and calls that overlap in time need one each.  L2L_E_STATE if another device than the context's is current.
+
+   Dropout masks are a function of (seed, site, element) and are never stored: the generator is Philox-4x32 with seven
+   rounds (Salmon et al., SC 2011), key = seed, counter words 2 and 3 = site (low, high).  Use another site for
+   every place that drops, and another seed or site for every step and micro-batch; a layer recomputed with the same pair sees the same
+   mask.  step: device uint64 or NULL; its value when the kernel runs is added to site, so that a captured
+   launch takes another mask when the program has counted it up between replays (forward and backward with the same value). */
+
+/* Attention over `sequences` sequences in token-major rows.  Sequence b owns the rows first[b] .. first[b] + len[b] - 1 of every
+   matrix (device int32 arrays; NULL: first[b] = b max_len, len[b] = max_len), of length 0 to max_len, anywhere in
+   rows 0 .. rows - 1: padded batches, packed ones, and any mixture (sequences must not overlap).  Rows of no
+   sequence are neither read nor written.  A sequence that does not fit rows or max_len is skipped, and the next l2l_sync returns L2L_E_ARG. */
+typedef struct {
+  int dtype;             /* of all matrices */
+  int heads, kv_heads;   /* query heads; key and value heads: head h reads head h / (heads / kv_heads) */
+  int head_dim;          /* d: multiple of 8, 8 .. 128 */
+  int sequences, max_len;   /* max_len <= 262144 */
+  long long rows;        /* token rows of the matrices */
+  const int32_t* first;
+  const int32_t* len;
+  int causal;            /* 1: a query sees the keys up to its own position; 0: all of its sequence */
+  float scale;           /* > 0: factor on the scores, 1 / sqrt(d) as a rule */
+  double dropout;        /* share of the probabilities that is dropped (the others are divided by the kept share); to the
+                            nearest 1/256, one random byte a probability: byte 4 (i % 4) + j % 4 of the call with counter words 0, 1 =
+                            (i / 4) << 16 | j / 4, 2^31 | (b heads + h) for query i, key j of sequence b and head h is kept if >= 256 p */
+  uint64_t seed, site;
+  const uint64_t* step;
+} l2l_attention;
+/* o = (softmax(scale q k^T) dropped) v.  q, o: [rows, heads d], k, v: [rows, kv_heads d], each with its own row stride in elements (column
+   groups of one QKV matrix do); 16-byte aligned, strides too.  lse: float [heads][rows], the logarithm of each softmax
+   row's denominator (NULL: not wanted; the backward call needs it).  work: l2l_op_attention_work_bytes bytes, 16-byte aligned, or NULL. */
+int l2l_op_attention(l2l_ctx*, const l2l_attention*, const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv,
+                     void* o, long long ldo, float* lse, void* work);
+/* Its gradients: dq [rows, heads d], dk, dv [rows, kv_heads d] (summed over the query heads that share them) from dout, the
+   gradient of o.  q, k, v, o, lse and the description as in the forward call; the probabilities are computed
+   again.  No atomics: the same call gives the same bits.  Outputs must not overlap inputs.  work: required. */
+int l2l_op_attention_bwd(l2l_ctx*, const l2l_attention*, const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv,
+                         const void* o, long long ldo, const float* lse, const void* dout, long long lddo, void* dq, long long lddq,
+                         void* dk, long long lddk, void* dv, long long lddv, void* work);
+/* 0 on a bad description. */
+size_t l2l_op_attention_work_bytes(const l2l_attention*);
+
+/* y = resid + drop(x + bias), [rows, n] with row strides in elements of any alignment; bias [n] and resid may be NULL; in
+   place (y = x or y = resid, same stride) allowed.  p: share of the elements that is dropped (the others are divided by
+   the kept share), to the nearest 1/65536: 16 random bits an element, half-word j % 8 (low half of word 0 first) of the call with
+   counter words 0, 1 = j / 8, i for element (i, j), kept if >= 65536 p. */
+int l2l_op_dropout(l2l_ctx*, int dtype, int rows, int n, const void* x, long long ldx, const void* bias, const void* resid, long long ldr,
+                   void* y, long long ldy, double p, uint64_t seed, uint64_t site, const uint64_t* step);
+/* dx = drop(dy) with the forward call's p, seed, site and step (the gradient of x; that of resid is dy).  dbias: float [n] or NULL,
+   receives the column sums of dx before their rounding (accumulate = 1: they are added to it); it needs work: l2l_op_dropout_work_bytes
+   bytes, 16-byte aligned.  In place allowed. */
+int l2l_op_dropout_bwd(l2l_ctx*, int dtype, int rows, int n, const void* dy, long long lddy, void* dx, long long lddx, double p, uint64_t seed,
+                       uint64_t site, const uint64_t* step, float* dbias, int accumulate, void* work);
+size_t l2l_op_dropout_work_bytes(int rows, int n);
+
+/* Of each row of logits ([rows, vocab], row stride ld in elements, any alignment), with p = softmax(row): logp = log p[ids[row]] (0 where
+   ids[row] < 0; an id of vocab or more is clamped, and the next l2l_sync returns L2L_E_ARG), entropy = -sum p log p, lse
+   = log sum e^x, and the `top` (0 .. 32) most probable tokens: top_ids int32 [rows][top], top_logp float [rows][top], most probable
+   first, equal ones by lowest id.  ids and logp may both be NULL.  Logits of -inf have probability 0; a row of nothing else gives lse =
+   logp = top_logp = -inf and entropy 0.  A row with NaN or +inf gives NaN.  work: l2l_op_token_logprobs_work_bytes bytes (may be 0),
+   16-byte aligned, or NULL, which leaves calls of few rows to one workgroup each. */
+int l2l_op_token_logprobs(l2l_ctx*, int dtype, int rows, int vocab, const void* logits, long long ld, const int32_t* ids, float* logp,
+                          float* entropy, float* lse, int top, int32_t* top_ids, float* top_logp, void* work);
+/* dlogits ([rows, vocab], row stride ldd, dtype of the logits; in place allowed) from the gradients of logp and of entropy (float [rows],
+   either may be NULL = zero); lse and entropy as the forward call left them.  Rows of nothing but -inf get zeros. */
+int l2l_op_token_logprobs_bwd(l2l_ctx*, int dtype, int rows, int vocab, const void* logits, long long ld, const int32_t* ids, const float* lse,
+                              const float* entropy, const float* dlogp, const float* dentropy, void* dlogits, long long ldd);
+size_t l2l_op_token_logprobs_work_bytes(int rows, int vocab, int top);
+
 /* ---- host EPS (Section 2.1, 2.3): fp32 master weights + Adam on host cores ---------------------- */
 typedef struct eps_store eps_store;
 /* n_blocks parameter blocks with elems[i] packed elements each.  ship_dtype: dtype of the copy that

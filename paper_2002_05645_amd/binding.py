@@ -26,6 +26,12 @@ class l2l_config(C.Structure):
                 ("ln_eps", C.c_float), ("vocab", C.c_int), ("ubatch_group", C.c_int)]
 
 
+class l2l_attention(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("heads", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("sequences", C.c_int),
+                ("max_len", C.c_int), ("rows", C.c_longlong), ("first", C.c_void_p), ("len", C.c_void_p), ("causal", C.c_int),
+                ("scale", C.c_float), ("dropout", C.c_double), ("seed", C.c_uint64), ("site", C.c_uint64), ("step", C.c_void_p)]
+
+
 class L2LError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"l2l error {code}: {msg}")
@@ -36,6 +42,8 @@ _lib = None
 
 _P = C.c_void_p
 _CFGP = C.POINTER(l2l_config)
+_ATTP = C.POINTER(l2l_attention)
+_LL = C.c_longlong
 _SIGS = {
     "l2l_layer_tensor_count": (C.c_int, []),
     "l2l_embed_tensor_count": (C.c_int, []),
@@ -89,6 +97,15 @@ _SIGS = {
     "l2l_noalloc_scratch_bytes": (C.c_size_t, []),
     "l2l_noalloc_last_error": (C.c_char_p, []),
     "l2l_op_layernorm": (C.c_int, [_P, C.c_int, C.c_int, C.c_int, _P, _P, _P, C.c_float, _P, _P, _P]),
+    "l2l_op_attention": (C.c_int, [_P, _ATTP, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P, _P]),
+    "l2l_op_attention_bwd": (C.c_int, [_P, _ATTP, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P]),
+    "l2l_op_attention_work_bytes": (C.c_size_t, [_ATTP]),
+    "l2l_op_dropout": (C.c_int, [_P, C.c_int, C.c_int, C.c_int, _P, _LL, _P, _P, _LL, _P, _LL, C.c_double, C.c_uint64, C.c_uint64, _P]),
+    "l2l_op_dropout_bwd": (C.c_int, [_P, C.c_int, C.c_int, C.c_int, _P, _LL, _P, _LL, C.c_double, C.c_uint64, C.c_uint64, _P, _P, C.c_int, _P]),
+    "l2l_op_dropout_work_bytes": (C.c_size_t, [C.c_int, C.c_int]),
+    "l2l_op_token_logprobs": (C.c_int, [_P, C.c_int, C.c_int, C.c_int, _P, _LL, _P, _P, _P, _P, C.c_int, _P, _P, _P]),
+    "l2l_op_token_logprobs_bwd": (C.c_int, [_P, C.c_int, C.c_int, C.c_int, _P, _LL, _P, _P, _P, _P, _P, _P, _LL]),
+    "l2l_op_token_logprobs_work_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
     "eps_create": (C.c_int, [C.c_int, C.POINTER(C.c_size_t), C.c_int, C.c_int, C.POINTER(_P)]),
     "eps_destroy": (C.c_int, [_P]),
     "eps_master": (C.POINTER(C.c_float), [_P, C.c_int]),
@@ -147,6 +164,36 @@ def lib():
 def make_config(hidden, heads, ffn, seq, ubatch, num_ubatches, dtype, ln_eps=1e-12, vocab=0, ubatch_group=0):
     d = DTYPES.get(dtype, dtype)
     return l2l_config(hidden, heads, ffn, seq, ubatch, num_ubatches, d, ln_eps, vocab, ubatch_group)
+
+
+def make_attention(*, dtype, heads, head_dim, sequences, max_len, rows=None, kv_heads=None, first=None, length=None, causal=False,
+                   scale=None, dropout=0.0, seed=0, site=0, step=None):
+    """Description of an attention call (l2l_attention).  first, length: int32 device tensors or None; step: a one-element int64 device
+    tensor or None; they are kept alive with the description.  Defaults: rows = sequences x max_len, kv_heads = heads, scale = 1 / sqrt(head_dim)."""
+    a = l2l_attention(DTYPES.get(dtype, dtype), heads, heads if kv_heads is None else kv_heads, head_dim, sequences, max_len,
+                      sequences * max_len if rows is None else rows, _ptr(first), _ptr(length), int(bool(causal)),
+                      max(1, head_dim) ** -0.5 if scale is None else scale, dropout, _u64(seed), _u64(site), _ptr(step))
+    a.tensors = (first, length, step)
+    return a
+
+
+def _u64(x):
+    return int(x) & 0xFFFFFFFFFFFFFFFF
+
+
+def attention_work_bytes(a):
+    """Bytes of workspace of the attention calls with this description; 0 for one that they refuse."""
+    return lib().l2l_op_attention_work_bytes(C.byref(a))
+
+
+def dropout_work_bytes(rows, n):
+    """Bytes of workspace of op_dropout_bwd with dbias."""
+    return lib().l2l_op_dropout_work_bytes(rows, n)
+
+
+def token_logprobs_work_bytes(rows, vocab, top=0):
+    """Bytes of workspace of op_token_logprobs (0: it needs none)."""
+    return lib().l2l_op_token_logprobs_work_bytes(rows, vocab, top)
 
 
 def layer_layout(cfg):
@@ -359,6 +406,30 @@ class Context:
     def op_layernorm(self, dtype, rows, n, x, gamma, beta, eps, y, mean=None, rstd=None):
         self._ck(lib().l2l_op_layernorm(self._h, dtype, rows, n, _ptr(x), _ptr(gamma), _ptr(beta), eps, _ptr(y),
                                         _ptr(mean), _ptr(rstd)))
+
+
+    def op_attention(self, attention, q, ldq, k, ldk, v, ldv, o, ldo, lse=None, work=None):
+        self._ck(lib().l2l_op_attention(self._h, C.byref(attention), _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(o), ldo, _ptr(lse), _ptr(work)))
+
+    def op_attention_bwd(self, attention, q, ldq, k, ldk, v, ldv, o, ldo, lse, dout, lddo, dq, lddq, dk, lddk, dv, lddv, work):
+        self._ck(lib().l2l_op_attention_bwd(self._h, C.byref(attention), _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(o), ldo, _ptr(lse),
+                                            _ptr(dout), lddo, _ptr(dq), lddq, _ptr(dk), lddk, _ptr(dv), lddv, _ptr(work)))
+
+    def op_dropout(self, dtype, rows, n, x, ldx, y, ldy, p, seed, site, bias=None, resid=None, ldr=0, step=None):
+        self._ck(lib().l2l_op_dropout(self._h, dtype, rows, n, _ptr(x), ldx, _ptr(bias), _ptr(resid), ldr, _ptr(y), ldy, p, _u64(seed), _u64(site),
+                                      _ptr(step)))
+
+    def op_dropout_bwd(self, dtype, rows, n, dy, lddy, dx, lddx, p, seed, site, dbias=None, work=None, accumulate=False, step=None):
+        self._ck(lib().l2l_op_dropout_bwd(self._h, dtype, rows, n, _ptr(dy), lddy, _ptr(dx), lddx, p, _u64(seed), _u64(site), _ptr(step), _ptr(dbias),
+                                          int(accumulate), _ptr(work)))
+
+    def op_token_logprobs(self, dtype, rows, vocab, logits, ld, ids, logp, entropy, lse, top=0, top_ids=None, top_logp=None, work=None):
+        self._ck(lib().l2l_op_token_logprobs(self._h, dtype, rows, vocab, _ptr(logits), ld, _ptr(ids), _ptr(logp), _ptr(entropy), _ptr(lse), top,
+                                             _ptr(top_ids), _ptr(top_logp), _ptr(work)))
+
+    def op_token_logprobs_bwd(self, dtype, rows, vocab, logits, ld, ids, lse, entropy, dlogp, dentropy, dlogits, ldd):
+        self._ck(lib().l2l_op_token_logprobs_bwd(self._h, dtype, rows, vocab, _ptr(logits), ld, _ptr(ids), _ptr(lse), _ptr(entropy), _ptr(dlogp),
+                                                 _ptr(dentropy), _ptr(dlogits), ldd))
 
 
 class EPS:

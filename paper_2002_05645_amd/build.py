@@ -19,6 +19,7 @@ HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
              "-Wno-unused-result"] + os.environ.get("L2L_EXTRA_HIPFLAGS", "").split()   # (experiments: extra -D switches)
 with open(os.path.join(CSRC, "gemm_variants.h")) as _f:
     NUM_GEMM_VARIANTS = int(re.search(r"kNumGemmVariants\s*=\s*(\d+)", _f.read()).group(1))
+SEQ_ATTN_WIDTHS = (32, 64, 96, 128)
 HOST_FLAGS = ["-O3", "-std=c++17", "-fPIC", "-mavx2", "-mfma", "-mf16c", "-fno-math-errno", "-fopenmp-simd",   # (sqrt without errno, simd reductions: the optimizer loops vectorise)
               "-D__HIP_PLATFORM_AMD__", f"-I{ROCM}/include", "-pthread"]
 
@@ -40,6 +41,14 @@ def build(verbose: bool = False) -> str:
     jobs = [[HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, "l2l.hip"), "-o", o_hip],
             ["g++", *HOST_FLAGS, "-c", os.path.join(CSRC, "eps.cpp"), "-o", o_eps]]
     objs = [o_hip, o_eps]
+    o_tok = os.path.join(obj_dir, "token_ops.o")
+    jobs.append([HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, "token_ops.hip"), "-o", o_tok])
+    objs.append(o_tok)
+    for width in SEQ_ATTN_WIDTHS:             # one per padded head width and element type (fp32, bf16, fp16)
+        for elem in range(3):
+            o = os.path.join(obj_dir, f"seq_attention_{elem}_{width}.o")
+            jobs.append([HIPCC, *HIP_FLAGS, f"-DL2L_DP={width}", f"-DL2L_ELEM={elem}", "-c", os.path.join(CSRC, "seq_attention_variant.hip"), "-o", o])
+            objs.append(o)
     for v in range(NUM_GEMM_VARIANTS):        # one translation unit per MFMA tile variant and 16-bit format
         for tag, extra in (("v", []), ("h", ["-DL2L_ELEM_FP16=1"])):
             o = os.path.join(obj_dir, f"gemm_{tag}{v}.o")

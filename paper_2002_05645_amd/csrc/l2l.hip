@@ -19,6 +19,7 @@
 #include "gemm_variants.h"
 #include "attention.h"
 #include "rowwise.h"
+#include "ops.h"
 
 // ================================================================================================
 // packed layouts (host only)
@@ -156,7 +157,8 @@ struct l2l_ctx {
   int copy_rows = 1;                        // drains issued as rows (DMA engine); L2L_COPY_ROWS=0: as plain copies (the runtime's copy kernel)
   int no_weight_transpose = 0;              // L2L_NO_WEIGHT_TRANSPOSE=1: forward GEMMs read W as stored ([in, out], K-strided B operand)
   int resident_cus = 0;                     // workgroups of a resident GEMM launch (CUs of the device; L2L_GEMM_RESIDENT=0: none)
-  int32_t* bad_ids = nullptr;               // device flag: a token id or label outside the vocabulary was seen
+  int32_t* bad_ids = nullptr;               // device flags: 1 a token id or label outside the vocabulary was seen, 2 a sequence outside its rows
+  int device = 0;                           // the device that was current when the context was created
   long long T = 0, Mg = 0;                  // tokens per micro-batch, rows per launch group
   size_t dev_bytes = 0;
   std::vector<void*> allocs;
@@ -1465,6 +1467,7 @@ int l2l_create(const l2l_config* cfg, void* compute_stream, void* copy_stream, l
     return L2L_E_HIP;
   }
   l2l_ctx* c = new l2l_ctx;
+  if (hipGetDevice(&c->device) != hipSuccess) { (void)hipGetLastError(); c->device = 0; }
   c->cfg = *cfg;
   c->lay = make_layout(cfg);
   c->cs = (hipStream_t)compute_stream;
@@ -1640,6 +1643,8 @@ int l2l_sync(l2l_ctx* c) {
     HIP_TRY(c, hipMemcpy(&bad, c->bad_ids, 4, hipMemcpyDeviceToHost));
     if (bad) {
       HIP_TRY(c, hipMemset(c->bad_ids, 0, 4));
+      if (bad == 2)
+        return fail(c, L2L_E_ARG, "l2l_op_attention: a sequence that does not fit the token rows or max_len was passed since the last l2l_sync; such sequences are skipped");
       return fail(c, L2L_E_ARG, "a token id or label outside its range (vocabulary %d, or the head's classes) was passed since the last l2l_sync; such ids are clamped and the results are not meaningful",
                   c->cfg.vocab);
     }
@@ -2308,6 +2313,223 @@ int l2l_op_layernorm(l2l_ctx* c, int dtype, int rows, int n, const void* x, cons
   if (dtype == L2L_FP16) return ln_fwd<fp16>(c, x, gamma, beta, y, mean, rstd, rows, n, eps);
   if (dtype == L2L_F32) return ln_fwd<float>(c, x, gamma, beta, y, mean, rstd, rows, n, eps);
   return fail(c, L2L_E_ARG, "l2l_op_layernorm: bad dtype");
+}
+
+// ================================================================================================
+// single operations of fine-tuning: attention over sequences of different lengths, dropout, token log probabilities
+// ================================================================================================
+// kernels go to the context's stream, which belongs to the device it was created on
+static int need_device(l2l_ctx* c, const char* who) {
+  int dev = 0;
+  HIP_TRY(c, hipGetDevice(&dev));
+  if (dev != c->device) return fail(c, L2L_E_STATE, "%s: device %d is current, the context belongs to device %d", who, dev, c->device);
+  return L2L_OK;
+}
+
+static bool dtype_ok(int dtype) { return dtype == L2L_F32 || is16(dtype); }
+
+// a probability as a threshold of `steps` (256 or 65536): the nearest one; false if that is 0 or all of them although p is neither
+static bool drop_threshold(double p, int steps, uint32_t* drop) {
+  if (!(p >= 0.0 && p < 1.0)) return false;
+  const double t = std::nearbyint(p * steps);
+  *drop = (uint32_t)t;
+  return p == 0.0 || (t >= 1.0 && t <= steps - 1.0);
+}
+
+static const char* attention_desc_error(const l2l_attention* a) {
+  uint32_t drop;
+  if (!a) return "null description";
+  if (!dtype_ok(a->dtype)) return "bad dtype";
+  if (a->heads <= 0 || a->kv_heads <= 0 || a->heads % a->kv_heads) return "heads must be a multiple of kv_heads, both positive";
+  if (a->head_dim < 8 || a->head_dim > 128 || a->head_dim % 8) return "head_dim must be a multiple of 8 from 8 to 128";
+  if (a->sequences < 0 || a->rows < 0 || a->max_len < 0 || a->max_len > 262144) return "sequences, rows and max_len (at most 262144) must not be negative";
+  if (!a->first && (long long)a->sequences * a->max_len > a->rows) return "without `first`, sequences x max_len must not exceed rows";
+  if (!(a->scale > 0.f) || !std::isfinite(a->scale)) return "scale must be positive and finite";
+  if (!drop_threshold(a->dropout, 256, &drop)) return "dropout must be 0, or from 1/512 to 511/512 (it is taken to the nearest 1/256)";
+  if (((uintptr_t)a->first | (uintptr_t)a->len) & 3 || (uintptr_t)a->step & 7) return "misaligned first, len or step";
+  if ((long long)a->sequences * a->heads * ((a->max_len + 31) / 32) > (1LL << 30)) return "too many (sequence, head, query block)s for one launch";
+  return nullptr;
+}
+
+size_t l2l_op_attention_work_bytes(const l2l_attention* a) {
+  if (attention_desc_error(a)) return 0;
+  return (size_t)a->heads * (size_t)a->rows * 8;
+}
+
+// rows of `heads` heads as the kernels read and write them
+static bool attention_rows_ok(const l2l_attention* a, const void* p, long long ld, int heads) {
+  const long long e = (long long)esize(a->dtype);
+  return p && !((uintptr_t)p & 15) && ld * e % 16 == 0 && ld >= (long long)heads * a->head_dim && ld * e * 64 < (1LL << 31);
+}
+
+static SeqAttnArgs attention_args(l2l_ctx* c, const l2l_attention* a, const void* q, long long ldq, const void* k, long long ldk, const void* v,
+                                  long long ldv) {
+  SeqAttnArgs g;
+  memset(&g, 0, sizeof(g));
+  g.q = q; g.k = k; g.v = v; g.ldq = ldq; g.ldk = ldk; g.ldv = ldv;
+  g.first = a->first; g.len = a->len;
+  g.heads = a->heads; g.kv_heads = a->kv_heads; g.d = a->head_dim; g.sequences = a->sequences; g.max_len = a->max_len; g.causal = a->causal != 0;
+  g.rows = a->rows; g.scale = a->scale;
+  (void)drop_threshold(a->dropout, 256, &g.drop);
+  g.seed = a->seed; g.site = a->site; g.step = a->step;
+  g.bad = c->bad_ids;
+  return g;
+}
+
+#define L2L_SEQ_ATTN_PICK(dir, dtype, d, args, s)                                            \
+  do {                                                                                       \
+    const int dp_ = ((d) + 31) / 32 * 32;                                                    \
+    void (*f_)(const SeqAttnArgs&, hipStream_t) = nullptr;                                   \
+    if (dp_ == 32) f_ = L2L_SEQ_ATTN_TYPES(dir, dtype, 32);                                  \
+    else if (dp_ == 64) f_ = L2L_SEQ_ATTN_TYPES(dir, dtype, 64);                             \
+    else if (dp_ == 96) f_ = L2L_SEQ_ATTN_TYPES(dir, dtype, 96);                             \
+    else f_ = L2L_SEQ_ATTN_TYPES(dir, dtype, 128);                                           \
+    f_(args, s);                                                                             \
+  } while (0)
+#define L2L_SEQ_ATTN_TYPES(dir, dtype, dp) \
+  ((dtype) == L2L_BF16 ? l2l_seq_attn_##dir##_v##dp : (dtype) == L2L_FP16 ? l2l_seq_attn_##dir##_h##dp : l2l_seq_attn_##dir##_f##dp)
+
+int l2l_op_attention(l2l_ctx* c, const l2l_attention* a, const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv,
+                     void* o, long long ldo, float* lse, void* work) {
+  if (!c) return L2L_E_ARG;
+  if (const char* e = attention_desc_error(a)) return fail(c, L2L_E_ARG, "l2l_op_attention: %s", e);
+  if (a->sequences == 0 || a->max_len == 0 || a->rows == 0) return L2L_OK;
+  if (!attention_rows_ok(a, q, ldq, a->heads) || !attention_rows_ok(a, k, ldk, a->kv_heads) || !attention_rows_ok(a, v, ldv, a->kv_heads) ||
+      !attention_rows_ok(a, o, ldo, a->heads))
+    return fail(c, L2L_E_ARG, "l2l_op_attention: q, k, v and o must be 16-byte aligned, with rows that are 16-byte multiples and hold every head (and 64 of them 2 GiB at most)");
+  if ((uintptr_t)lse & 3 || (uintptr_t)work & 15) return fail(c, L2L_E_ARG, "l2l_op_attention: misaligned lse or work");
+  if (o == q || o == k || o == v) return fail(c, L2L_E_ARG, "l2l_op_attention: o must not overlap an input");
+  L2L_TRY(need_device(c, "l2l_op_attention"));
+  SeqAttnArgs g = attention_args(c, a, q, ldq, k, ldk, v, ldv);
+  g.out = o; g.ldo = ldo; g.lse = lse;
+  return timed(c, L2L_PROF_ATTN, 0, 0, [&] { L2L_SEQ_ATTN_PICK(fwd, a->dtype, a->head_dim, g, c->cs); });
+}
+
+int l2l_op_attention_bwd(l2l_ctx* c, const l2l_attention* a, const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv,
+                         const void* o, long long ldo, const float* lse, const void* dout, long long lddo, void* dq, long long lddq, void* dk,
+                         long long lddk, void* dv, long long lddv, void* work) {
+  if (!c) return L2L_E_ARG;
+  if (const char* e = attention_desc_error(a)) return fail(c, L2L_E_ARG, "l2l_op_attention_bwd: %s", e);
+  if (a->sequences == 0 || a->max_len == 0 || a->rows == 0) return L2L_OK;
+  if (!attention_rows_ok(a, q, ldq, a->heads) || !attention_rows_ok(a, k, ldk, a->kv_heads) || !attention_rows_ok(a, v, ldv, a->kv_heads) ||
+      !attention_rows_ok(a, o, ldo, a->heads) || !attention_rows_ok(a, dout, lddo, a->heads) || !attention_rows_ok(a, dq, lddq, a->heads) ||
+      !attention_rows_ok(a, dk, lddk, a->kv_heads) || !attention_rows_ok(a, dv, lddv, a->kv_heads))
+    return fail(c, L2L_E_ARG, "l2l_op_attention_bwd: every matrix must be 16-byte aligned, with rows that are 16-byte multiples and hold every head (and 64 of them 2 GiB at most)");
+  if (!lse || (uintptr_t)lse & 3 || !work || (uintptr_t)work & 15) return fail(c, L2L_E_ARG, "l2l_op_attention_bwd: null or misaligned lse or work");
+  for (const void* out : {dq, dk, dv})
+    for (const void* in : {q, k, v, o, dout})
+      if (out == in) return fail(c, L2L_E_ARG, "l2l_op_attention_bwd: dq, dk and dv must not overlap an input");
+  if (dq == dk || dq == dv || dk == dv) return fail(c, L2L_E_ARG, "l2l_op_attention_bwd: dq, dk and dv must not overlap");
+  L2L_TRY(need_device(c, "l2l_op_attention_bwd"));
+  SeqAttnArgs g = attention_args(c, a, q, ldq, k, ldk, v, ldv);
+  g.o = o; g.ldo = ldo; g.lse = (float*)lse; g.dout = dout; g.lddo = lddo;
+  g.dq = dq; g.lddq = lddq; g.dk = dk; g.lddk = lddk; g.dv = dv; g.lddv = lddv;
+  g.nlse2 = (float*)work;
+  g.delta = g.nlse2 + (long long)a->heads * a->rows;
+  return timed(c, L2L_PROF_ATTN, 0, 0, [&] { L2L_SEQ_ATTN_PICK(bwd, a->dtype, a->head_dim, g, c->cs); });
+}
+
+static bool dropout_rows_ok(int dtype, const void* p, long long ld, int n) { return p && (uintptr_t)p % esize(dtype) == 0 && ld >= n; }
+
+size_t l2l_op_dropout_work_bytes(int rows, int n) { return rows > 0 && n > 0 ? (size_t)dropout_row_blocks(rows, n) * (size_t)n * 4 : 0; }
+
+// what both directions check; drop receives the threshold
+static int dropout_check(l2l_ctx* c, const char* who, int dtype, int rows, int n, const void* x, long long ldx, const void* y, long long ldy, double p,
+                         const uint64_t* step, uint32_t* drop) {
+  if (!dtype_ok(dtype)) return fail(c, L2L_E_ARG, "%s: bad dtype", who);
+  if (rows < 0 || n < 0) return fail(c, L2L_E_ARG, "%s: negative size", who);
+  if (!drop_threshold(p, 65536, drop)) return fail(c, L2L_E_ARG, "%s: p must be 0, or from 2^-17 to 1 - 2^-17 (it is taken to the nearest 1/65536)", who);
+  if ((uintptr_t)step & 7) return fail(c, L2L_E_ARG, "%s: misaligned step", who);
+  if (rows == 0 || n == 0) return L2L_OK;
+  if (!dropout_rows_ok(dtype, x, ldx, n) || !dropout_rows_ok(dtype, y, ldy, n))
+    return fail(c, L2L_E_ARG, "%s: null or misaligned pointer, or rows shorter than n", who);
+  if (x == y && ldx != ldy) return fail(c, L2L_E_ARG, "%s: in place needs equal row strides", who);
+  return need_device(c, who);
+}
+
+int l2l_op_dropout(l2l_ctx* c, int dtype, int rows, int n, const void* x, long long ldx, const void* bias, const void* resid, long long ldr, void* y,
+                   long long ldy, double p, uint64_t seed, uint64_t site, const uint64_t* step) {
+  if (!c) return L2L_E_ARG;
+  DropoutArgs g;
+  memset(&g, 0, sizeof(g));
+  L2L_TRY(dropout_check(c, "l2l_op_dropout", dtype, rows, n, x, ldx, y, ldy, p, step, &g.drop));
+  if (rows == 0 || n == 0) return L2L_OK;
+  if (bias && (uintptr_t)bias % esize(dtype)) return fail(c, L2L_E_ARG, "l2l_op_dropout: misaligned bias");
+  if (resid && !dropout_rows_ok(dtype, resid, ldr, n)) return fail(c, L2L_E_ARG, "l2l_op_dropout: misaligned resid, or its rows shorter than n");
+  if (resid == y && resid && ldr != ldy) return fail(c, L2L_E_ARG, "l2l_op_dropout: in place needs equal row strides");
+  g.x = x; g.ldx = ldx; g.bias = bias; g.resid = resid; g.ldr = ldr; g.y = y; g.ldy = ldy; g.rows = rows; g.n = n;
+  g.seed = seed; g.site = site; g.step = step;
+  return timed(c, L2L_PROF_ROWWISE, 0, (resid ? 3.0 : 2.0) * rows * n * esize(dtype), [&] { l2l_launch_dropout(g, dtype, c->cs); });
+}
+
+int l2l_op_dropout_bwd(l2l_ctx* c, int dtype, int rows, int n, const void* dy, long long lddy, void* dx, long long lddx, double p, uint64_t seed,
+                       uint64_t site, const uint64_t* step, float* dbias, int accumulate, void* work) {
+  if (!c) return L2L_E_ARG;
+  DropoutArgs g;
+  memset(&g, 0, sizeof(g));
+  L2L_TRY(dropout_check(c, "l2l_op_dropout_bwd", dtype, rows, n, dy, lddy, dx, lddx, p, step, &g.drop));
+  if (dbias && ((uintptr_t)dbias & 3 || !work || (uintptr_t)work & 15)) return fail(c, L2L_E_ARG, "l2l_op_dropout_bwd: misaligned dbias, or null or misaligned work");
+  if (n == 0) return L2L_OK;
+  if (rows == 0) {   // the sum over no rows
+    if (!dbias || accumulate) return L2L_OK;
+    L2L_TRY(need_device(c, "l2l_op_dropout_bwd"));
+    return fill_zero(c, dbias, (size_t)n * 4);
+  }
+  g.x = dy; g.ldx = lddy; g.y = dx; g.ldy = lddx; g.rows = rows; g.n = n;
+  g.seed = seed; g.site = site; g.step = step; g.dbias = dbias; g.part = (float*)work; g.accumulate = accumulate != 0;
+  return timed(c, L2L_PROF_ROWWISE, 0, 2.0 * rows * n * esize(dtype), [&] { l2l_launch_dropout(g, dtype, c->cs); });
+}
+
+constexpr int kMaxTop = 32;
+
+size_t l2l_op_token_logprobs_work_bytes(int rows, int vocab, int top) {
+  if (rows <= 0 || vocab <= 0 || vocab > (1 << 30) || top < 0 || top > kMaxTop) return 0;
+  return logprob_work_bytes(rows, logprob_splits(rows, vocab), top);
+}
+
+static int logprob_check(l2l_ctx* c, const char* who, int dtype, int rows, int vocab, const void* logits, long long ld, const int32_t* ids) {
+  if (!dtype_ok(dtype)) return fail(c, L2L_E_ARG, "%s: bad dtype", who);
+  if (rows < 0 || vocab <= 0 || vocab > (1 << 30)) return fail(c, L2L_E_ARG, "%s: rows must not be negative, vocab from 1 to 2^30", who);
+  if ((long long)rows * ((vocab + 1023) / 1024 + 32) > (1LL << 31) - 1) return fail(c, L2L_E_ARG, "%s: rows x vocab too large for one launch", who);
+  if (rows == 0) return L2L_OK;
+  if (!logits || (uintptr_t)logits % esize(dtype) || ld < vocab) return fail(c, L2L_E_ARG, "%s: null or misaligned logits, or rows shorter than vocab", who);
+  if ((uintptr_t)ids & 3) return fail(c, L2L_E_ARG, "%s: misaligned ids", who);
+  return need_device(c, who);
+}
+
+int l2l_op_token_logprobs(l2l_ctx* c, int dtype, int rows, int vocab, const void* logits, long long ld, const int32_t* ids, float* logp, float* entropy,
+                          float* lse, int top, int32_t* top_ids, float* top_logp, void* work) {
+  if (!c) return L2L_E_ARG;
+  L2L_TRY(logprob_check(c, "l2l_op_token_logprobs", dtype, rows, vocab, logits, ld, ids));
+  if (top < 0 || top > kMaxTop || top > vocab) return fail(c, L2L_E_ARG, "l2l_op_token_logprobs: top must be from 0 to 32, and at most vocab");
+  if (rows == 0) return L2L_OK;
+  if ((ids == nullptr) != (logp == nullptr)) return fail(c, L2L_E_ARG, "l2l_op_token_logprobs: ids and logp go together");
+  if (!entropy || !lse || (top && (!top_ids || !top_logp))) return fail(c, L2L_E_ARG, "l2l_op_token_logprobs: null output");
+  if (((uintptr_t)logp | (uintptr_t)entropy | (uintptr_t)lse | (uintptr_t)top_ids | (uintptr_t)top_logp) & 3 || (uintptr_t)work & 15)
+    return fail(c, L2L_E_ARG, "l2l_op_token_logprobs: misaligned output or work");
+  LogprobArgs g;
+  memset(&g, 0, sizeof(g));
+  g.logits = logits; g.ld = ld; g.ids = ids; g.rows = rows; g.vocab = vocab; g.top = top;
+  g.logp = logp; g.entropy = entropy; g.lse = lse; g.top_ids = top_ids; g.top_logp = top_logp;
+  g.work = work; g.splits = work ? logprob_splits(rows, vocab) : 1; g.bad = c->bad_ids;
+  return timed(c, L2L_PROF_OTHER, 0, (double)rows * vocab * esize(dtype), [&] { l2l_launch_logprobs(g, dtype, c->cs); });
+}
+
+int l2l_op_token_logprobs_bwd(l2l_ctx* c, int dtype, int rows, int vocab, const void* logits, long long ld, const int32_t* ids, const float* lse,
+                              const float* entropy, const float* dlogp, const float* dentropy, void* dlogits, long long ldd) {
+  if (!c) return L2L_E_ARG;
+  L2L_TRY(logprob_check(c, "l2l_op_token_logprobs_bwd", dtype, rows, vocab, logits, ld, ids));
+  if (rows == 0) return L2L_OK;
+  if (!lse || !dlogits || (uintptr_t)dlogits % esize(dtype) || ldd < vocab) return fail(c, L2L_E_ARG, "l2l_op_token_logprobs_bwd: null lse, or null or misaligned dlogits, or its rows shorter than vocab");
+  if (dlogp && !ids) return fail(c, L2L_E_ARG, "l2l_op_token_logprobs_bwd: dlogp needs ids");
+  if (dentropy && !entropy) return fail(c, L2L_E_ARG, "l2l_op_token_logprobs_bwd: dentropy needs entropy");
+  if (((uintptr_t)lse | (uintptr_t)entropy | (uintptr_t)dlogp | (uintptr_t)dentropy) & 3) return fail(c, L2L_E_ARG, "l2l_op_token_logprobs_bwd: misaligned input");
+  if (dlogits == logits && ldd != ld) return fail(c, L2L_E_ARG, "l2l_op_token_logprobs_bwd: in place needs equal row strides");
+  LogprobArgs g;
+  memset(&g, 0, sizeof(g));
+  g.logits = logits; g.ld = ld; g.ids = ids; g.rows = rows; g.vocab = vocab;
+  g.lse = (float*)lse; g.entropy = (float*)entropy; g.dlogp = dlogp; g.dentropy = dentropy; g.dlogits = dlogits; g.ldd = ldd;
+  return timed(c, L2L_PROF_OTHER, 0, 2.0 * rows * vocab * esize(dtype), [&] { l2l_launch_logprobs_bwd(g, dtype, c->cs); });
 }
 
 }  // extern "C"

@@ -1,0 +1,63 @@
+// Attention over sequences of different lengths for one element type and padded head width (-DL2L_DP=32, 64, 96 or 128; -DL2L_ELEM=0 fp32,
+// 1 bf16, 2 fp16): each pair is a translation unit of its own, so that the build runs in parallel.
+#if L2L_ELEM == 0
+#include "seq_attention_f32.h"
+#else
+#include "seq_attention.h"
+#endif
+
+#define L2L_CAT2(a, b) a##b
+#define L2L_CAT(a, b) L2L_CAT2(a, b)
+#if L2L_ELEM == 0
+typedef float Elem;
+#define L2L_NAME(x) L2L_CAT(L2L_CAT(x, f), L2L_DP)
+#elif L2L_ELEM == 1
+typedef bf16 Elem;
+#define L2L_NAME(x) L2L_CAT(L2L_CAT(x, v), L2L_DP)
+#else
+typedef fp16 Elem;
+#define L2L_NAME(x) L2L_CAT(L2L_CAT(x, h), L2L_DP)
+#endif
+
+namespace {
+
+// one workgroup per `rows_per` rows of every (sequence, head), rounded up to a multiple of the 8 XCDs
+dim3 blocks(const SeqAttnArgs& a, int heads, int rows_per) {
+  const long long n = (long long)a.sequences * heads * ((a.max_len + rows_per - 1) / rows_per);
+  return dim3((unsigned)((n + 7) / 8 * 8));
+}
+
+template <typename K>
+void go(K kern, dim3 grid, const SeqAttnArgs& a, hipStream_t s) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a); }
+
+}  // namespace
+
+void L2L_NAME(l2l_seq_attn_fwd_)(const SeqAttnArgs& a, hipStream_t s) {
+#if L2L_ELEM == 0
+  if (a.drop) go(sattn::seq_fwd_f32_kernel<L2L_DP, true>, blocks(a, a.heads, 128), a, s);
+  else go(sattn::seq_fwd_f32_kernel<L2L_DP, false>, blocks(a, a.heads, 128), a, s);
+#else
+  if (a.drop) go(sattn::seq_fwd_kernel<Elem, L2L_DP, 1, true>, blocks(a, a.heads, 128), a, s);
+  else go(sattn::seq_fwd_kernel<Elem, L2L_DP, 1, false>, blocks(a, a.heads, 128), a, s);
+#endif
+}
+
+void L2L_NAME(l2l_seq_attn_bwd_)(const SeqAttnArgs& a, hipStream_t s) {
+#if L2L_ELEM == 0
+  if (a.drop) {
+    go(sattn::seq_bwd_dq_f32_kernel<L2L_DP, true>, blocks(a, a.heads, 128), a, s);
+    go(sattn::seq_bwd_dkv_f32_kernel<L2L_DP, true>, blocks(a, a.kv_heads, 128), a, s);
+  } else {
+    go(sattn::seq_bwd_dq_f32_kernel<L2L_DP, false>, blocks(a, a.heads, 128), a, s);
+    go(sattn::seq_bwd_dkv_f32_kernel<L2L_DP, false>, blocks(a, a.kv_heads, 128), a, s);
+  }
+#else
+  if (a.drop) {
+    go(sattn::seq_bwd_dq_kernel<Elem, L2L_DP, true>, blocks(a, a.heads, 128), a, s);
+    go(sattn::seq_bwd_dkv_kernel<Elem, L2L_DP, true>, blocks(a, a.kv_heads, 128), a, s);
+  } else {
+    go(sattn::seq_bwd_dq_kernel<Elem, L2L_DP, false>, blocks(a, a.heads, 128), a, s);
+    go(sattn::seq_bwd_dkv_kernel<Elem, L2L_DP, false>, blocks(a, a.kv_heads, 128), a, s);
+  }
+#endif
+}
