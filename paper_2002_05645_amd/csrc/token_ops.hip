@@ -119,18 +119,34 @@ __global__ __launch_bounds__(256) void dropout_kernel(const DropoutArgs a, int c
   }
 }
 
-// dbias (+)= the partial sums: 16 columns a workgroup, 16 lanes to a column
+// dbias (+)= the partial sums: 16 columns a workgroup, four to a thread, 64 lanes down the blocks; bound by the latency of one
+// round of loads, so a thread asks for eight at a time
 __global__ __launch_bounds__(256) void dropout_sum_kernel(const float* part, int blocks, int n, float* dbias, int accumulate) {
-  __shared__ float red[16][17];
-  const int c = threadIdx.x & 15, l = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
-  float s = 0.f;
-  if (col < n)
-    for (int b = l; b < blocks; b += 16) s += part[(long long)b * n + col];
-  red[l][c] = s;
+  __shared__ float red[64][17];
+  const int c = (threadIdx.x & 3) * 4, l = threadIdx.x >> 2, col = blockIdx.x * 16 + c, count = min(4, n - col);
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int b0 = l; b0 < blocks && count > 0; b0 += 64 * 8) {
+    float v[8][4];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int b = b0 + 64 * u;
+        v[u][i] = b < blocks && i < count ? part[(long long)b * n + col + i] : 0.f;
+      }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] += v[u][i];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) red[l][c + i] = s[i];
   __syncthreads();
-  if (l == 0 && col < n) {
-    for (int j = 1; j < 16; ++j) s += red[j][c];
-    dbias[col] = accumulate ? dbias[col] + s : s;
+  if (threadIdx.x < 16 && blockIdx.x * 16 + threadIdx.x < n) {
+    const int at = blockIdx.x * 16 + threadIdx.x;
+    float t = 0.f;
+    for (int j = 0; j < 64; ++j) t += red[j][threadIdx.x];
+    dbias[at] = accumulate ? dbias[at] + t : t;
   }
 }
 
@@ -150,33 +166,36 @@ void launch_dropout_t(const DropoutArgs& a, hipStream_t s) {
 }
 
 // ---- token log probabilities ---------------------------------------------------------------------------------------------
-// Of a row of logits x: m = max, s = sum e^(x - m), t = sum e^(x - m) (x - m); lse = m + log s, log p(id) = x[id] - m - log s, entropy
-// = log s - t / s, and the `top` largest by (value, lowest index first).  One pass over memory: a workgroup holds a slab of the row in
+// Of a row of logits x, with m = max, s = sum e^(x - m), t = sum e^(x - m) (x - m): lse = m + log s, log p(id) = x[id] - m - log s, entropy
+// = log s - t / s; and the `top` largest by (value, lowest index first).  One pass over memory: a workgroup holds a slab of the row in
 // registers, from which it takes the sums and the candidates for the top.  A value can be among the top k only if it is not
 // below the k-th largest of any 64 values of the row; each wave takes that bound from its lanes' own maxima (a binary search by
-// ballots over their leading bits), the workgroup the highest of them, and what reaches it (some dozens of the slab) goes to a list in LDS,
-// where every candidate counts how many are before it: its place.  Where equal values overflow the list, the workgroup searches the top one by one.
+// ballots over their leading bits), and what reaches the highest bound known goes to a list in LDS: some dozens of the row, of
+// which each counts in the end how many are before it, its place.  Where equal values overflow the list, the workgroup searches the top one by one.
 // Bound by memory: two workgroups of 512 threads share a compute unit and load under each other's reductions.
 // Rows too few to fill the chip are split over workgroups, whose parts a second kernel joins.
-constexpr int LP_NT = 512, LP_WAVES = LP_NT / 64, LP_LIST = 1024, LP_TOP = 32;
-constexpr float LP_FAR = -1.0e4f;   // e^x is 0 from here down, and 0 * x has to be 0 as well for x = -inf
+constexpr int LP_LIST = 1024, LP_TOP = 32;
+constexpr float LP_FAR = -1.0e4f;   // 2^x is 0 from here down, and 0 * x has to be 0 as well for x = -inf
+constexpr float LP_LOG2E = 1.4426950408889634f, LP_LN2 = 0.6931471805599453f;
 
-// whole numbers in the order of the values (-0 and 0 alike)
+// whole numbers in the order of the values (-0 and 0 alike, every NaN before everything)
 __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.0f);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  return x != x ? 0xFFFFFFFFu : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
 // larger = earlier in the top: the value, then the lower index
 __device__ __forceinline__ uint64_t rank_key(uint32_t key, uint32_t index) { return (uint64_t)key << 32 | (0xFFFFFFFFu - index); }
 
+// In powers of two: m = the largest x log2(e), s = sum 2^(x log2(e) - m), t = sum 2^(..) (x log2(e) - m).  (m may be rounded: every
+// exponent is taken against the same rounded one, in one fma.)
 struct Stat { float m, s, t; };
 // both relative to their own maximum; an empty one (m = -inf, s = t = 0) changes nothing
 __device__ __forceinline__ Stat join(Stat a, Stat b) {
   Stat r;
   r.m = fmaxf(a.m, b.m);
   if (r.m == -INFINITY) return Stat{r.m, a.s + b.s, a.t + b.t};
-  const float da = fmaxf(a.m - r.m, LP_FAR), db = fmaxf(b.m - r.m, LP_FAR), fa = __expf(da), fb = __expf(db);
+  const float da = fmaxf(a.m - r.m, LP_FAR), db = fmaxf(b.m - r.m, LP_FAR), fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
   r.s = a.s * fa + b.s * fb;
   r.t = (a.t + a.s * da) * fa + (b.t + b.s * db) * fb;
   return r;
@@ -184,160 +203,243 @@ __device__ __forceinline__ Stat join(Stat a, Stat b) {
 __device__ __forceinline__ Stat wave_join(Stat a) {
   Stat r;
   r.m = wave_max(a.m);
-  const float d = r.m == -INFINITY ? 0.f : fmaxf(a.m - r.m, LP_FAR), f = __expf(d);
+  const float d = r.m == -INFINITY ? 0.f : fmaxf(a.m - r.m, LP_FAR), f = __builtin_amdgcn_exp2f(d);
   r.s = wave_sum(a.s * f);
   r.t = wave_sum((a.t + a.s * d) * f);
   return r;
 }
 
-__device__ __forceinline__ void write_row(const LogprobArgs& a, int row, Stat st, float x_id) {
-  const bool none = st.m == -INFINITY;   // every logit is -inf
-  const float log_s = logf(st.s);
-  a.lse[row] = none ? -INFINITY : st.m + log_s;
-  a.entropy[row] = none ? 0.f : log_s - st.t / st.s;
-  if (a.ids) a.logp[row] = a.ids[row] < 0 ? 0.f : none ? -INFINITY : (x_id - st.m) - log_s;
+// each lane's entry to its place among the first `found` lanes' if that is one of the `top` first
+__device__ __forceinline__ void place_64(uint64_t k, int found, int lane, int top, uint64_t* best) {
+  int before = 0;
+  for (int o = 0; o < found; ++o) {
+    const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), o) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)k, o);
+    before += other > k;
+  }
+  if (lane < found && before < top) best[before] = k;
 }
 
-template <typename T, int NV>
-__global__ __launch_bounds__(LP_NT) __attribute__((amdgpu_waves_per_eu(4)))
+// the largest number, to 13 leading bits, that `count` lanes' keys reach
+__device__ __forceinline__ uint32_t lanes_reach(uint32_t key, int count) {
+  uint32_t reach = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 19; --bit)
+    if (__popcll(__ballot(key >= (reach | 1u << bit))) >= count) reach |= 1u << bit;
+  return reach;
+}
+
+// log p of a logit x of the row
+__device__ __forceinline__ float log_prob(Stat st, float x) {
+  return st.m == -INFINITY ? -INFINITY : (fmaf(x, LP_LOG2E, -st.m) - log2f(st.s)) * LP_LN2;
+}
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int row, Stat st, int id, float x_id) {
+  const bool none = st.m == -INFINITY;   // every logit is -inf
+  const float log_s = log2f(st.s);
+  a.lse[row] = none ? -INFINITY : (st.m + log_s) * LP_LN2;
+  a.entropy[row] = none ? 0.f : (log_s - st.t / st.s) * LP_LN2;
+  if (id >= a.vocab) atomicOr(a.bad, 1);   // (clamped)
+  if (a.ids) a.logp[row] = id < 0 ? 0.f : log_prob(st, x_id);
+}
+
+// NT threads, NV lines of 16 bytes each; AHEAD: for rows of several slabs, the next one's lines on their way while one is worked on (else
+// the slab is the whole range), and the next row's behind the last slab; TINY: vocabularies shorter than a line
+template <typename T, int NT, int NV, bool AHEAD, bool TINY = false>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4)))
 void logprob_kernel(const LogprobArgs a) {
-  constexpr int N = Line<T>::N, SLAB = LP_NT * N * NV;
-  __shared__ uint64_t list[LP_LIST], best[LP_TOP];
-  __shared__ Stat wave_stat[LP_WAVES];
-  __shared__ uint32_t bound[LP_WAVES];
-  __shared__ int count;
-  const int row = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+  constexpr int N = Line<T>::N, SLAB = NT * N * NV, WAVES = NT / 64;
+  static_assert(N * NV <= 64, "a thread's values are bits of a word");
+  __shared__ uint64_t lists[AHEAD ? 2 : 1][LP_LIST], best[LP_TOP];   // (two lists, taken in turn: a wave may be a row ahead of another)
+  __shared__ Stat wave_stat[WAVES];
+  __shared__ int counts[2];
+  __shared__ uint32_t bounds[2], wave_bound[WAVES];
+  const int split = blockIdx.x % a.splits, stride = gridDim.x / a.splits;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, top = a.top;
-  // splits of whole slabs' worth of threads' chunks, so that all but the last one are full
+  // (splits begin at whole lines, so that all but the last one are of equal length)
   const int chunks = (a.vocab + N - 1) / N, per_split = (chunks + a.splits - 1) / a.splits * N;
-  const int begin = min(a.vocab, split * per_split), end = min(a.vocab, begin + per_split);
-  const T* x = (const T*)a.logits + (long long)row * a.ld;
-  float x_id = 0.f;
-  if (tid == 0 && split == 0 && a.ids) {
-    int id = a.ids[row];
-    if (id >= a.vocab) { atomicOr(a.bad, 1); id = a.vocab - 1; }
-    if (id >= 0) x_id = to_f32(x[id]);
-  }
-  Stat st = {-INFINITY, 0.f, 0.f};
-  int have = 0;                // entries of list that earlier slabs left, in order
-  uint32_t floor_key = 0;      // the top-th of them, once there are as many
-  for (int slab = begin; slab < end; slab += SLAB) {
-    float v[NV][N];
+  const int begin = min(a.vocab, split * per_split), end = min(a.vocab, begin + per_split), last = max(0, end - N);
+  // Every line is loaded, the last whole one of the range where a thread's own would pass the end (no branch between the
+  // loads, so that all are under way at once); what it holds of other threads' values becomes -inf.
+  using Line16 = Vec16<T, N>;
+  Line16 r[NV], next[AHEAD ? NV : 1];
+  const auto load = [&](Line16 (&to)[NV], const T* x, int from) {
+    if constexpr (!TINY) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int at = slab + (j * LP_NT + tid) * N;
-      if (at + N <= end) {
-        const Vec16<T, N> r = *(const Vec16<T, N>*)(x + at);
+      for (int j = 0; j < NV; ++j) to[j] = *(const Line16*)(x + min(from + (j * NT + tid) * N, last));
+    } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[j][i] = to_f32(r.v[i]);
-      } else {
+      for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[j][i] = at + i < end ? to_f32(x[at + i]) : -INFINITY;
-      }
+        for (int i = 0; i < N; ++i) to[j].v[i] = i < a.vocab ? x[i] : from_f32<T>(-INFINITY);
     }
-    float lm = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < N; ++i) lm = fmaxf(lm, v[j][i]);
-    Stat mine = {lm, 0.f, 0.f};
-    const float base = lm == -INFINITY ? 0.f : lm;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float d = v[j][i] - base, e = __expf(d);
-        mine.s += e;
-        mine.t = fmaf(e, fmaxf(d, LP_FAR), mine.t);
+  };
+  int row = blockIdx.x / a.splits;
+  load(r, (const T*)a.logits + (long long)row * a.ld, begin);
+  if (tid < 2) { counts[tid] = 0; bounds[tid] = 0; }
+  if (top) __syncthreads();
+  int turn = 0;
+  do {
+    const T* x = (const T*)a.logits + (long long)row * a.ld;
+    // (through the scalar cache, and its logit by every thread: neither is waited for before the lines, and the logit not before the end)
+    const int id = a.ids ? *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.ids + row) : -1;
+    const float x_id = to_f32(x[max(0, min(id, a.vocab - 1))]);
+    uint64_t* list = lists[turn];
+    Stat st = {-INFINITY, 0.f, 0.f};   // of this wave's values
+    for (int slab = begin; slab < end; slab += SLAB) {
+      // (behind the last row's last slab every thread asks for one line of it: under a condition, the loads of both paths would be waited for here)
+      if constexpr (AHEAD) {
+        const bool more = slab + SLAB < end, rows = row + stride < a.rows;
+        load(next, more || !rows ? x : x + (long long)stride * a.ld, more ? slab + SLAB : rows ? begin : end);
       }
-    const Stat w = wave_join(mine);
-    // the largest bound, to 16 leading bits, that `top` lanes' maxima reach
-    uint32_t reach = 0;
-    if (top) {
-      const uint32_t key = order_key(lm);
+      int own0 = slab + tid * N;
+      const auto own = [&](int j) { return own0 + j * NT * N; };   // the first index this thread answers for,
+      const auto at = [&](int j) { return min(own(j), last); };    // and where its line starts
+      float lm = -INFINITY;
 #pragma unroll
-      for (int bit = 31; bit >= 16; --bit)
-        if (__popcll(__ballot(key >= (reach | 1u << bit))) >= top) reach |= 1u << bit;
-    }
-    if (lane == 0) { wave_stat[wave] = w; bound[wave] = reach; }
-    if (tid == 0) count = have;
-    __syncthreads();
-    for (int j = 0; j < LP_WAVES; ++j) st = join(st, wave_stat[j]);
-    if (top) {
-      uint32_t least = floor_key;
+      for (int j = 0; j < NV; ++j) {
+        if (own(j) + N > end) {
 #pragma unroll
-      for (int j = 0; j < LP_WAVES; ++j) least = max(least, bound[j]);
-      if (order_key(lm) >= least) {   // (few threads)
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const uint32_t key = order_key(v[j][i]), at = slab + (j * LP_NT + tid) * N + i;
-            if (key >= least && at < (uint32_t)end) {
-              const int slot = atomicAdd(&count, 1);
-              if (slot < LP_LIST) list[slot] = rank_key(key, at);
-            }
-          }
-      }
-      __syncthreads();
-      const int found = count;
-      if (found <= LP_LIST) {
-        for (int u = tid; u < found; u += LP_NT) {
-          const uint64_t k = list[u];
-          int before = 0;
-          for (int o = 0; o < found; ++o) before += list[o] > k;
-          if (before < top) best[before] = k;
+          for (int i = 0; i < N; ++i)
+            if (at(j) + i < own(j)) r[j].v[i] = from_f32<T>(-INFINITY);
         }
-        have = min(found, top);
-      } else {
-        // one by one: the largest after the previous one, over the slab and what earlier slabs left
-        const int earlier = have;
-        uint64_t prev = ~0ull;
-        have = 0;
-        while (have < top) {
-          uint64_t k = tid < earlier && list[tid] < prev ? list[tid] : 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) lm = fmaxf(lm, to_f32(r[j].v[i]));
+      }
+      // (what is derived from the values is derived again where it is used next: kept, it would take a multiple of their registers)
+      const auto forget = [&] {
+        asm("" : "+v"(own0));
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          u32x4 raw = __builtin_bit_cast(u32x4, r[j]);
+          asm("" : "+v"(raw));
+          r[j] = __builtin_bit_cast(Line16, raw);
+        }
+      };
+      forget();
+      Stat mine = {lm == -INFINITY ? lm : lm * LP_LOG2E, 0.f, 0.f};
+      const float base = lm == -INFINITY ? 0.f : mine.m;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float d = fmaf(to_f32(r[j].v[i]), LP_LOG2E, -base), e = __builtin_amdgcn_exp2f(d);
+          mine.s += e;
+          mine.t = fmaf(e, fmaxf(d, LP_FAR), mine.t);
+        }
+      st = join(st, wave_join(mine));
+      if (top) {
+        // The bound may be any that is one: if each of t waves has q lanes whose maxima reach b, and t q >= top, then b is.  The first
+        // slab's is the t-th largest of the waves' own, each the largest, to 13 leading bits, that q lanes reach; with q near top / (half
+        // the waves) it leaves a fraction of the candidates that the best wave's alone would (q = top).  Behind it waves
+        // raise it by that one, and read it, without waiting for each other.
+        const uint32_t key = order_key(lm);
+        uint32_t least;
+        if (slab == begin) {
+          const int half = max(1, min(WAVES, (end - begin + 64 * N - 1) / (64 * N)) / 2);   // (of the waves that have values)
+          const int q = (top + half - 1) / half, t = (top + q - 1) / q;
+          const uint32_t reach = lanes_reach(key, q);
+          if (lane == 0) wave_bound[wave] = reach;
+          __syncthreads();
+          const uint32_t b = lane < WAVES ? wave_bound[lane] : 0;
+          int reached_by = 0;
+#pragma unroll
+          for (int o = 0; o < WAVES; ++o) reached_by += (uint32_t)__builtin_amdgcn_readlane((int)b, o) >= b;
+          const uint32_t cand = reached_by >= t ? b : 0;
+          least = 0;
+#pragma unroll
+          for (int o = 0; o < WAVES; ++o) least = max(least, (uint32_t)__builtin_amdgcn_readlane((int)cand, o));
+          if (tid == 0) atomicMax(&bounds[turn], least);
+        } else {
+          least = *(volatile uint32_t*)&bounds[turn];
+          if (__popcll(__ballot(key > least)) >= top) {
+            const uint32_t reach = lanes_reach(key, top);
+            if (lane == 0) atomicMax(&bounds[turn], reach);
+            least = max(least, reach);
+          }
+        }
+        const float least_value = key_value(least);
+        if (!(lm < least_value)) {   // (few threads)
+          // which of the lines' values, as bits; then one at a time, read again (a line's place in registers cannot be computed)
+          forget();
+          uint64_t reached = 0;
 #pragma unroll
           for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-              const uint32_t at = slab + (j * LP_NT + tid) * N + i;
-              const uint64_t o = rank_key(order_key(v[j][i]), at);
-              if (at < (uint32_t)end && o < prev && o > k) k = o;
+            for (int i = 0; i < N; ++i) reached |= (uint64_t)!(to_f32(r[j].v[i]) < least_value) << (j * N + i);
+          while (reached) {
+            const int e = __builtin_ctzll(reached), index = at(e / N) + e % N;
+            reached &= reached - 1;
+            if (index >= own(e / N) && index < end) {
+              const int slot = atomicAdd(&counts[turn], 1);
+              if (slot < LP_LIST) list[slot] = rank_key(order_key(to_f32(x[index])), (uint32_t)index);
             }
+          }
+        }
+      }
+      if constexpr (AHEAD) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) r[j] = next[j];
+      }
+    }
+    if (lane == 0) wave_stat[wave] = st;
+    __syncthreads();
+    st = wave_stat[0];
+    for (int j = 1; j < WAVES; ++j) st = join(st, wave_stat[j]);
+    if (tid == 0) { counts[turn ^ 1] = 0; bounds[turn ^ 1] = 0; }
+    int have = 0;
+    if (top) {
+      const int found = counts[turn];
+      have = min(found, top);
+      if (found <= 64) {   // (one wave, whose lanes read each other)
+        if (wave == 0) place_64(lane < found ? list[lane] : 0, found, lane, top, best);
+      } else if (found <= LP_LIST) {
+        for (int u = tid; u < found; u += NT) {
+          const uint64_t k = list[u];
+          int before = 0;
+#pragma unroll 8
+          for (int o = 0; o < found; ++o) before += list[o] > k;
+          if (before < top) best[before] = k;
+        }
+      } else {
+        // too many equal ones: one by one, the largest after the previous one, from memory
+        uint64_t prev = ~0ull;
+        for (int n = 0; n < top; ++n) {
+          uint64_t k = 0;
+          for (int index = begin + tid; index < end; index += NT) {
+            const uint64_t o = rank_key(order_key(to_f32(x[index])), (uint32_t)index);
+            if (o < prev && o > k) k = o;
+          }
 #pragma unroll
           for (int off = 32; off; off >>= 1) {
             const uint64_t o = (uint64_t)__shfl_xor((unsigned)(k >> 32), off, 64) << 32 | __shfl_xor((unsigned)k, off, 64);
             k = o > k ? o : k;
           }
-          __syncthreads();   // (the slots at the end of the list, past what earlier slabs left, carry the waves' results)
-          if (lane == 0) list[LP_LIST - LP_WAVES + wave] = k;
           __syncthreads();
-          for (int j = 0; j < LP_WAVES; ++j) k = max(k, list[LP_LIST - LP_WAVES + j]);
-          if (tid == 0) best[have] = k;
-          ++have;
+          if (lane == 0) list[wave] = k;
+          __syncthreads();
+          for (int j = 0; j < WAVES; ++j) k = max(k, list[j]);
+          if (tid == 0) best[n] = k;
           prev = k;
         }
       }
-      __syncthreads();
-      if (tid < have) list[tid] = best[tid];
-      floor_key = have == top ? (uint32_t)(best[top - 1] >> 32) : 0;
     }
-    __syncthreads();   // the list and the waves' results are free again, and what is left of the list can be read
-  }
-  if (a.splits == 1) {
-    if (tid == 0) write_row(a, row, st, x_id);
-    if (tid < top) {
-      const uint64_t k = list[tid];
-      a.top_ids[(long long)row * top + tid] = (int32_t)(0xFFFFFFFFu - (uint32_t)k);
-      a.top_logp[(long long)row * top + tid] = st.m == -INFINITY ? -INFINITY : (key_value((uint32_t)(k >> 32)) - st.m) - logf(st.s);
+    __syncthreads();
+    if (a.splits == 1) {
+      if (tid == 0) write_row(a, row, st, id, x_id);
+      if (tid < top) {
+        const uint64_t k = best[tid];
+        a.top_ids[(long long)row * top + tid] = (int32_t)(0xFFFFFFFFu - (uint32_t)k);
+        a.top_logp[(long long)row * top + tid] = log_prob(st, key_value((uint32_t)(k >> 32)));
+      }
+    } else {
+      // [rows][splits] of: m, s, t, x[id]; then `top` ranks (fewer: zeros, which are behind everything)
+      float* part = (float*)a.work + ((long long)row * a.splits + split) * 4;
+      uint64_t* ranks = (uint64_t*)((float*)a.work + (long long)a.rows * a.splits * 4) + ((long long)row * a.splits + split) * top;
+      if (tid == 0) { part[0] = st.m; part[1] = st.s; part[2] = st.t; part[3] = x_id; }
+      if (tid < top) ranks[tid] = tid < have ? best[tid] : 0;
     }
-  } else {
-    // [rows][splits] of: m, s, t, x[id]; then `top` ranks (fewer: zeros, which are behind everything)
-    float* part = (float*)a.work + ((long long)row * a.splits + split) * 4;
-    uint64_t* ranks = (uint64_t*)((float*)a.work + (long long)a.rows * a.splits * 4) + ((long long)row * a.splits + split) * top;
-    if (tid == 0) { part[0] = st.m; part[1] = st.s; part[2] = st.t; part[3] = x_id; }
-    if (tid < top) ranks[tid] = tid < have ? list[tid] : 0;
-  }
+    row += stride;
+    turn ^= 1;
+  } while (AHEAD && row < a.rows);
 }
 
 __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs a) {
@@ -349,14 +451,14 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs a) 
   Stat st = {-INFINITY, 0.f, 0.f};
   for (int j = 0; j < a.splits; ++j) st = join(st, Stat{part[4 * j], part[4 * j + 1], part[4 * j + 2]});
   __syncthreads();
-  if (tid == 0) write_row(a, row, st, part[3]);
+  if (tid == 0) write_row(a, row, st, a.ids ? a.ids[row] : -1, part[3]);
   for (int u = tid; u < n; u += 256) {
     const uint64_t k = list[u];
     int before = 0;
     for (int o = 0; o < n; ++o) before += list[o] > k;
     if (k && before < top) {
       a.top_ids[(long long)row * top + before] = (int32_t)(0xFFFFFFFFu - (uint32_t)k);
-      a.top_logp[(long long)row * top + before] = st.m == -INFINITY ? -INFINITY : (key_value((uint32_t)(k >> 32)) - st.m) - logf(st.s);
+      a.top_logp[(long long)row * top + before] = log_prob(st, key_value((uint32_t)(k >> 32)));
     }
   }
 }
@@ -400,12 +502,22 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(const LogprobArgs a, i
 template <typename T>
 void launch_logprobs_t(const LogprobArgs& a, hipStream_t s) {
   constexpr int N = Line<T>::N;
-  const dim3 grid((unsigned)((long long)a.rows * a.splits));
   const int per = (a.vocab + a.splits - 1) / a.splits + N;
-  // registers for the slab by what a workgroup has to hold: 32768 values at most at a time
-  if (per <= LP_NT * N) hipLaunchKernelGGL((logprob_kernel<T, 1>), grid, dim3(LP_NT), 0, s, a);
-  else if (per <= LP_NT * 16) hipLaunchKernelGGL((logprob_kernel<T, 16 / N>), grid, dim3(LP_NT), 0, s, a);
-  else hipLaunchKernelGGL((logprob_kernel<T, 64 / N>), grid, dim3(LP_NT), 0, s, a);
+  const long long wgs = (long long)a.rows * a.splits;
+  const auto go = [&](auto kern, int threads, long long most = 1LL << 31) {
+    hipLaunchKernelGGL(kern, dim3((unsigned)std::min(wgs, most)), dim3(threads), 0, s, a);
+  };
+  if (a.vocab < N) go(logprob_kernel<T, 512, 1, false, true>, 512);
+  else if (wgs > 256) {   // two workgroups of 512 threads to a compute unit
+    if (per <= 512 * N) go(logprob_kernel<T, 512, 1, false>, 512);
+    else if (per <= 512 * 16) go(logprob_kernel<T, 512, 16 / N, false>, 512);
+    else if (N == 4 && per <= 512 * 64) go(logprob_kernel<T, 512, 64 / N, false>, 512);
+    else go(logprob_kernel<T, 512, 8, true>, 512, a.splits == 1 ? 512 : wgs);
+  } else {              // a compute unit to each: as many threads as fit one workgroup
+    if (per <= 1024 * N) go(logprob_kernel<T, 1024, 1, false>, 1024);
+    else if (per <= 1024 * 32) go(logprob_kernel<T, 1024, 32 / N, false>, 1024);
+    else go(logprob_kernel<T, 1024, 8, true>, 1024);
+  }
   if (a.splits > 1) hipLaunchKernelGGL(logprob_join_kernel, dim3(a.rows), dim3(256), 0, s, a);
 }
 
@@ -426,8 +538,7 @@ void l2l_launch_dropout(const DropoutArgs& a, int dtype, hipStream_t s) {
 }
 
 int logprob_splits(int rows, int vocab) {
-  // as many as give 256 compute units a workgroup each, of 2048 values or more, and 32 at most (32 parts of 32 fill the joining list)
-  const int want = (256 + rows - 1) / rows, most = std::max(1, vocab / 2048);
+  const int want = (256 + rows - 1) / rows, most = std::max(1, vocab / 32768);
   return std::max(1, std::min(std::min(want, most), 32));
 }
 size_t logprob_work_bytes(int rows, int splits, int top) {
