@@ -1,6 +1,7 @@
 // Dropout with bias and residual, and token log probabilities with entropy and top alternatives: kernels and launchers of the
 // single operations that pass over memory once (entry points and checks: l2l.hip).
 #include <algorithm>
+#include <type_traits>
 
 #include "dropout.h"
 #include "ops.h"
@@ -19,134 +20,145 @@ struct Line {
 // ---- dropout -------------------------------------------------------------------------------------------------------------
 // y = resid + Z (x + bias); backward dx = Z dy and the column sums of dx (the bias gradient).  Z = 0 or 1 / kept share from
 // the generator in dropout.h: 16 bits an element, eight neighbours of a row from one call, nothing stored.
-// Bound by memory.  A thread owns eight columns and walks every (256 / CW)-th row of a block of rows, four rows requested at a
-// time; CW threads lie along the columns.  The column sums stay in fp32 registers, then add up across the workgroup's row lanes and leave as
+// Bound by memory.  A thread owns eight columns and walks every (256 / CW)-th row of a block of rows, up to four rows requested at
+// a time; CW threads lie along the columns.  The column sums stay in fp32 registers, then add up across the workgroup's row lanes and leave as
 // one row of partial sums per block, which a second kernel adds in a fixed order: no atomics, so the same call gives the same bits.
-constexpr int DROP_ROWS = 4;      // rows in flight per thread
 
 struct DropGrid { int cw, lanes, groups, per, blocks; };   // threads along columns, row lanes, column groups, rows per thread, row blocks
 DropGrid drop_grid(int rows, int n) {
   DropGrid g;
   const int chunks = (n + 7) / 8;
-  g.cw = 1;
-  while (g.cw < chunks && g.cw < 64) g.cw *= 2;
+  // threads along the columns: a power of two up to 64, the one that leaves the fewest without columns
+  const auto covered = [&](int cw) { return (long long)(chunks + cw - 1) / cw * cw; };
+  g.cw = 64;
+  for (int cw = 32; cw >= std::min(16, chunks); cw /= 2)
+    if (covered(cw) < covered(g.cw)) g.cw = cw;
   g.lanes = 256 / g.cw;
   g.groups = (chunks + g.cw - 1) / g.cw;
-  // rows per thread: as many as leave two thousand workgroups, at most 16 (the partial sums are then a sixtieth of the traffic at most)
-  const long long threads_rows = (long long)rows * g.groups / g.lanes / 2048;
-  g.per = (int)std::min<long long>(16, std::max<long long>(1, threads_rows));
-  g.per = g.per > DROP_ROWS ? (g.per + DROP_ROWS - 1) / DROP_ROWS * DROP_ROWS : g.per;
+  // rows per thread: 1, 2 or a multiple of 4, as many as leave two thousand workgroups, at most 16 (the partial sums are then a
+  // sixtieth of the traffic at most)
+  const long long share = (long long)rows * g.groups / g.lanes / 2048;
+  g.per = share >= 4 ? (int)std::min<long long>(16, share / 4 * 4) : share >= 2 ? 2 : 1;
   g.blocks = (rows + g.lanes * g.per - 1) / (g.lanes * g.per);
   return g;
 }
 
-template <typename T>
-__device__ __forceinline__ void load_cols(const T* p, int count, float (&v)[8]) {
-  if (count >= 8) {
-    const Vec16<T, 8> x = *(const Vec16<T, 8>*)p;
+// v[i] = v[i + by], 0 <= by < 8 (what comes from behind is not looked at)
+__device__ __forceinline__ void move_down(float (&v)[8], int by) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = to_f32(x.v[i]);
-  } else {
+  for (int step = 4; step; step >>= 1)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < count ? to_f32(p[i]) : 0.f;
-  }
-}
-template <typename T>
-__device__ __forceinline__ void store_cols(T* p, int count, const float (&v)[8]) {
-  if (count >= 8) {
-    Vec16<T, 8> x;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x.v[i] = from_f32<T>(v[i]);
-    *(Vec16<T, 8>*)p = x;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < count) p[i] = from_f32<T>(v[i]);
-  }
+    for (int i = 0; i + step < 8; ++i) v[i] = by & step ? v[i + step] : v[i];
 }
 
-template <typename T, bool RESID, bool SUMS>
-__global__ __launch_bounds__(256) void dropout_kernel(const DropoutArgs a, int cw, int lanes, int groups, int per) {
+// ROWS: rows in flight per thread
+template <typename T, int ROWS, bool RESID, bool SUMS, bool TINY>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4)))
+void dropout_kernel(const DropoutArgs a, int cw, int lanes, int groups, int per) {
+  using Line8 = Vec16<T, 8>;
   const int group = blockIdx.x % groups, block = blockIdx.x / groups;
   const int chunk = group * cw + threadIdx.x % cw, row_lane = threadIdx.x / cw, col = chunk * 8;
   const int count = min(8, a.n - col);   // <= 0: this thread has no columns
+  // Every line of every row is loaded, without a branch between the loads: a thread whose own would pass the end of the row takes the
+  // row's last eight columns and moves its own to the front (TINY, fewer than eight in all: one by one), one whose row would pass
+  // the last row takes that.
+  const int at = min(col, a.n - 8), by = min(7, col - at);
   const long long row0 = (long long)block * lanes * per + row_lane;
   const DropKey key = drop_key(a.seed, a.site, a.step);
   const float kept = 65536.0f / (65536.0f - (float)a.drop);
+  const auto load = [&](const void* base, long long row, long long ld) {
+    const T* p = (const T*)base + row * ld;
+    Line8 x;
+    if constexpr (TINY) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x.v[i] = p[min(i, a.n - 1)];
+    } else {
+      x = *(const Line8*)(p + at);
+    }
+    return x;
+  };
+  const auto widen = [&](const Line8& x, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_f32(x.v[i]);
+    if (!TINY && by) move_down(v, by);
+  };
   float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, sums[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (a.bias && count > 0) load_cols((const T*)a.bias + col, count, bias);
-  if (count > 0) {
-    for (int j = 0; j < per; j += DROP_ROWS) {
-      float x[DROP_ROWS][8], res[RESID ? DROP_ROWS : 1][8];
-      bool live[DROP_ROWS];
+  if (a.bias) widen(load(a.bias, 0, 0), bias);
+  for (int j = 0; j < per; j += ROWS) {
+    Line8 x[ROWS], res[RESID ? ROWS : 1];
 #pragma unroll
-      for (int u = 0; u < DROP_ROWS; ++u) {
-        const long long row = row0 + (long long)(j + u) * lanes;
-        live[u] = j + u < per && row < a.rows;
-        if (live[u]) {
-          load_cols((const T*)a.x + row * a.ldx + col, count, x[u]);
-          if (RESID) load_cols((const T*)a.resid + row * a.ldr + col, count, res[u]);
-        }
+    for (int u = 0; u < ROWS; ++u) {
+      const long long row = min(row0 + (long long)(j + u) * lanes, (long long)a.rows - 1);
+      x[u] = load(a.x, row, a.ldx);
+      if constexpr (RESID) res[u] = load(a.resid, row, a.ldr);
+    }
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+      const long long row = row0 + (long long)(j + u) * lanes;
+      const bool live = row < a.rows;
+      const u32x4 w = philox7((uint32_t)chunk, (uint32_t)row, key);
+      float v[8], r[8];
+      widen(x[u], v);
+      if constexpr (RESID) widen(res[u], r);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t bits = (w[i >> 1] >> (16 * (i & 1))) & 0xFFFFu;
+        const float z = bits >= a.drop ? (v[i] + bias[i]) * kept : 0.f;
+        if (SUMS) sums[i] += live ? z : 0.f;
+        v[i] = RESID ? r[i] + z : z;
       }
+      if (!live) continue;
+      T* out = (T*)a.y + row * a.ldy + col;
+      if (count >= 8) {
+        Line8 y;
 #pragma unroll
-      for (int u = 0; u < DROP_ROWS; ++u) {
-        if (!live[u]) continue;
-        const long long row = row0 + (long long)(j + u) * lanes;
-        const u32x4 w = philox7((uint32_t)chunk, (uint32_t)row, key);
+        for (int i = 0; i < 8; ++i) y.v[i] = from_f32<T>(v[i]);
+        *(Line8*)out = y;
+      } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t bits = (w[i >> 1] >> (16 * (i & 1))) & 0xFFFFu;
-          const float v = x[u][i] + bias[i];
-          const float z = bits >= a.drop ? v * kept : 0.f;
-          if (SUMS) sums[i] += z;
-          x[u][i] = RESID ? res[u][i] + z : z;
-        }
-        store_cols((T*)a.y + row * a.ldy + col, count, x[u]);
+        for (int i = 0; i < 7; ++i)
+          if (i < count) out[i] = from_f32<T>(v[i]);
       }
     }
   }
-  if (SUMS) {
+  if constexpr (SUMS) {
     __shared__ float red[256][9];   // (9: the eight values of 64 lanes spread over the banks)
 #pragma unroll
     for (int i = 0; i < 8; ++i) red[threadIdx.x][i] = sums[i];
     __syncthreads();
     for (int u = threadIdx.x; u < cw * 8; u += 256) {
-      const int c = u / 8, i = u % 8, at = (group * cw + c) * 8 + i;
+      const int c = u / 8, i = u % 8, to = (group * cw + c) * 8 + i;
       float s = 0.f;
       for (int l = 0; l < lanes; ++l) s += red[l * cw + c][i];
-      if (at < a.n) a.part[(long long)block * a.n + at] = s;
+      if (to < a.n) a.part[(long long)block * a.n + to] = s;
     }
   }
 }
 
-// dbias (+)= the partial sums: 16 columns a workgroup, four to a thread, 64 lanes down the blocks; bound by the latency of one
-// round of loads, so a thread asks for eight at a time
-__global__ __launch_bounds__(256) void dropout_sum_kernel(const float* part, int blocks, int n, float* dbias, int accumulate) {
-  __shared__ float red[64][17];
-  const int c = (threadIdx.x & 3) * 4, l = threadIdx.x >> 2, col = blockIdx.x * 16 + c, count = min(4, n - col);
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int b0 = l; b0 < blocks && count > 0; b0 += 64 * 8) {
-    float v[8][4];
+// dbias (+)= the partial sums: 16 columns a workgroup, 64 lanes down the blocks.  Bound by the latency of one round of loads (eight
+// at a time, unconditional ones: places past the end are read again and count nothing) and of the sum over the lanes.
+constexpr int DROP_SUM_NT = 1024;
+__global__ __launch_bounds__(DROP_SUM_NT) void dropout_sum_kernel(const float* part, int blocks, int n, float* dbias, int accumulate) {
+  __shared__ float red[64][17], red2[16][17];
+  const int c = threadIdx.x & 15, l = threadIdx.x >> 4, col = blockIdx.x * 16 + c, from = min(col, n - 1);
+  const float old = accumulate ? dbias[from] : 0.f;
+  float s = 0.f;
+  for (int b0 = l; b0 < blocks; b0 += 64 * 8) {
+    float v[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
+    for (int u = 0; u < 8; ++u) v[u] = part[(long long)min(b0 + 64 * u, blocks - 1) * n + from];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int b = b0 + 64 * u;
-        v[u][i] = b < blocks && i < count ? part[(long long)b * n + col + i] : 0.f;
-      }
-#pragma unroll
-    for (int u = 0; u < 8; ++u)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] += v[u][i];
+    for (int u = 0; u < 8; ++u) s += b0 + 64 * u < blocks ? v[u] : 0.f;
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) red[l][c + i] = s[i];
+  red[l][c] = s;
   __syncthreads();
-  if (threadIdx.x < 16 && blockIdx.x * 16 + threadIdx.x < n) {
-    const int at = blockIdx.x * 16 + threadIdx.x;
-    float t = 0.f;
-    for (int j = 0; j < 64; ++j) t += red[j][threadIdx.x];
-    dbias[at] = accumulate ? dbias[at] + t : t;
+  if (l < 16) red2[l][c] = (red[4 * l][c] + red[4 * l + 1][c]) + (red[4 * l + 2][c] + red[4 * l + 3][c]);
+  __syncthreads();
+  if (l == 0 && col < n) {
+    s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) s += red2[j][c];
+    dbias[col] = old + s;
   }
 }
 
@@ -155,13 +167,20 @@ void launch_dropout_t(const DropoutArgs& a, hipStream_t s) {
   const DropGrid g = drop_grid(a.rows, a.n);
   const dim3 grid((unsigned)((long long)g.groups * g.blocks));
   const auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a, g.cw, g.lanes, g.groups, g.per); };
+  const auto rows = [&](auto resid, auto sums) {
+    constexpr bool R = decltype(resid)::value, S = decltype(sums)::value;
+    if (a.n < 8) go(dropout_kernel<T, 1, R, S, true>);
+    else if (g.per >= 4) go(dropout_kernel<T, 4, R, S, false>);
+    else if (g.per == 2) go(dropout_kernel<T, 2, R, S, false>);
+    else go(dropout_kernel<T, 1, R, S, false>);
+  };
   if (a.dbias) {
-    go(dropout_kernel<T, false, true>);
-    hipLaunchKernelGGL(dropout_sum_kernel, dim3((a.n + 15) / 16), dim3(256), 0, s, a.part, g.blocks, a.n, a.dbias, a.accumulate);
+    rows(std::false_type{}, std::true_type{});
+    hipLaunchKernelGGL(dropout_sum_kernel, dim3((a.n + 15) / 16), dim3(DROP_SUM_NT), 0, s, a.part, g.blocks, a.n, a.dbias, a.accumulate);
   } else if (a.resid) {
-    go(dropout_kernel<T, true, false>);
+    rows(std::true_type{}, std::false_type{});
   } else {
-    go(dropout_kernel<T, false, false>);
+    rows(std::false_type{}, std::false_type{});
   }
 }
 
