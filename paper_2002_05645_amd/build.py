@@ -20,6 +20,8 @@ HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 with open(os.path.join(CSRC, "gemm_variants.h")) as _f:
     NUM_GEMM_VARIANTS = int(re.search(r"kNumGemmVariants\s*=\s*(\d+)", _f.read()).group(1))
 SEQ_ATTN_WIDTHS = (32, 64, 96, 128)
+# matrix products straight into vector registers, where the softmax works on them, instead of by way of the accumulation registers
+SEQ_ATTN_FLAGS = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 HOST_FLAGS = ["-O3", "-std=c++17", "-fPIC", "-mavx2", "-mfma", "-mf16c", "-fno-math-errno", "-fopenmp-simd",   # (sqrt without errno, simd reductions: the optimizer loops vectorise)
               "-D__HIP_PLATFORM_AMD__", f"-I{ROCM}/include", "-pthread"]
 
@@ -47,7 +49,7 @@ def build(verbose: bool = False) -> str:
     for width in SEQ_ATTN_WIDTHS:             # one per padded head width and element type (fp32, bf16, fp16)
         for elem in range(3):
             o = os.path.join(obj_dir, f"seq_attention_{elem}_{width}.o")
-            jobs.append([HIPCC, *HIP_FLAGS, f"-DL2L_DP={width}", f"-DL2L_ELEM={elem}", "-c", os.path.join(CSRC, "seq_attention_variant.hip"), "-o", o])
+            jobs.append([HIPCC, *HIP_FLAGS, *SEQ_ATTN_FLAGS, f"-DL2L_DP={width}", f"-DL2L_ELEM={elem}", "-c", os.path.join(CSRC, "seq_attention_variant.hip"), "-o", o])
             objs.append(o)
     for v in range(NUM_GEMM_VARIANTS):        # one translation unit per MFMA tile variant and 16-bit format
         for tag, extra in (("v", []), ("h", ["-DL2L_ELEM_FP16=1"])):

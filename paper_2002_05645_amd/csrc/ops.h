@@ -9,8 +9,8 @@ struct SeqAttnArgs {
   const void *q, *k, *v, *o, *dout;   // o, dout: backward only
   void *out, *dq, *dk, *dv;           // out: forward only
   float* lse;                         // [heads][rows]; written forward, read backward
-  float* nlse2;                       // backward, [heads][rows]: -lse log2(e) ...
-  float* delta;                       // ... and rowsum(dO O), left by the dQ kernel for the dK / dV kernel
+  float* nlse2;                       // backward, [heads][rows]: -lse / scale (16-bit formats) ...
+  float* delta;                       // ... and rowsum(dO O) (16-bit formats: negated), left by the dQ kernel for the dK / dV kernel
   long long ldq, ldk, ldv, ldo, lddo, lddq, lddk, lddv;   // row strides in elements
   const int32_t *first, *len;         // device, per sequence, or null
   int heads, kv_heads, d, sequences, max_len, causal;

@@ -11,6 +11,8 @@
 // dQ kernels, S = Q K^T with keys along the lanes in the dK / dV kernel, so that P and dS leave the accumulators as the B
 // operand of the next product.
 #pragma once
+#include <type_traits>
+
 #include "attention.h"
 #include "dropout.h"
 #include "ops.h"
@@ -77,6 +79,34 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[DP / 32], char* s
   }
 }
 
+// 64 rows of a matrix into an LDS image, 16 bytes a lane and instruction, by the four waves of a workgroup: the lanes' places within a tile
+// are worked out once, a tile moves only the descriptor.  Rows past the sequence and columns past the head lie outside the descriptor
+// and arrive as zeros.
+template <typename E, int DP>
+struct Tiles {
+  using I = Any<DP>;
+  static constexpr int PER = I::IMG / 4096;
+  const E* base;   // row 0 of the sequence, first column of the head
+  long long ld;
+  int n, d;
+  uint32_t off[PER];
+  __device__ __forceinline__ Tiles(const void* p, long long first, long long ld_, int head, int n_, int d_, int wave, int lane)
+      : base((const E*)p + first * ld_ + (long long)head * d_), ld(ld_), n(n_), d(d_) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int idx = (i * 4 + wave) * 64 + lane, row = idx / I::NC, c = I::chunk(row, idx % I::NC);
+      off[i] = c * 8 < d ? ((uint32_t)row * (uint32_t)ld + (uint32_t)c * 8) * 2u : BUF_OOB;
+    }
+  }
+  __device__ __forceinline__ void fetch(int row0, char* dst, int wave) const {
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(base + (long long)row0 * ld, (uint32_t)(((long long)(min(CHA, n - row0) - 1) * ld + d) * 2));
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(dst + (i * 4 + wave) * 1024), 16, (int)off[i], 0, 0, 0);
+  }
+};
+__device__ __forceinline__ f32x16 splat16(float x) { return f32x16{x, x, x, x, x, x, x, x, x, x, x, x, x, x, x, x}; }
+
 // ---- forward -----------------------------------------------------------------------------------------------------------
 // A workgroup owns 128 NQ queries of one (sequence, head), each of its four waves 32 NQ of them, and walks the keys in tiles of 64; the next
 // tile's K and V are on their way into the other half of the LDS while one is computed.
@@ -96,14 +126,12 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int q0 = base_q + wave * 32 * NQ;
   const bool active = q0 < n;   // (per wave)
-  const E* kb_ = (const E*)a.k + sq.first * a.ldk + (long long)hk * a.d;
-  const E* vb_ = (const E*)a.v + sq.first * a.ldv + (long long)hk * a.d;
+  const Tiles<E, DP> kt(a.k, sq.first, a.ldk, hk, n, a.d, wave, lane), vt(a.v, sq.first, a.ldv, hk, n, a.d, wave, lane);
   const int last = a.causal ? min(n, base_q + 128 * NQ) : n, tiles = (last + CHA - 1) / CHA;
   const auto fetch = [&](int t) {
     char* dst = lds + (t & 1) * 2 * I::IMG;
-    const int rows = min(CHA, n - t * CHA);
-    I::load(kb_ + (long long)t * CHA * a.ldk, (uint32_t)a.ldk, rows, a.d, dst, wave, lane);
-    I::load(vb_ + (long long)t * CHA * a.ldv, (uint32_t)a.ldv, rows, a.d, dst + I::IMG, wave, lane);
+    kt.fetch(t * CHA, dst, wave);
+    vt.fetch(t * CHA, dst + I::IMG, wave);
   };
   fetch(0);
   bf16x8 qf[NQ][DP / 16];
@@ -121,12 +149,13 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
   const float c = a.scale * LOG2E;
   DropKey key;
   if (DROP) key = drop_key(a.seed, a.site, a.step);
-  for (int t = 0; t < tiles; ++t) {
+  const auto arrive = [&](int t) {
     wait_vm0();
     __syncthreads();   // this tile is in, and every wave has left the one whose place the next one takes
     if (t + 1 < tiles) fetch(t + 1);
+  };
+  const auto compute = [&](int t, auto edge) {
     const int k0 = t * CHA;
-    if (!active || (a.causal && k0 >= q0 + 32 * NQ)) continue;
     const char* Ks = lds + (t & 1) * 2 * I::IMG;
     const char* Vs = Ks + I::IMG;
     f32x16 s[NQ][2];
@@ -141,7 +170,7 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
         for (int u = 0; u < NQ; ++u) s[u][kb] = mfma_32x32x16<E>(kf, qf[u][st], s[u][kb]);
       }
     }
-    if (k0 + CHA > n || (a.causal && k0 + CHA - 1 > q0)) {   // keys that a query does not see
+    if constexpr (decltype(edge)::value) {   // keys that a query does not see
 #pragma unroll
       for (int u = 0; u < NQ; ++u) {
         const int q = q0 + u * 32 + (lane & 31), lim = (a.causal ? min(n, q + 1) : n) - k0 - 4 * (lane >> 5);
@@ -202,7 +231,15 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
           for (int u = 0; u < NQ; ++u) o[u][t2] = mfma_32x32x16<E>(vf, pf[u], o[u][t2]);
         }
       }
-  }
+  };
+  // The wave's tiles: those that all of its queries see whole, those with a mask, and those of its neighbours', where it only helps to
+  // load.  In loops of their own: with the mask and the way round the work as branches inside one, the accumulators are copied back and forth.
+  const int mine = !active ? 0 : a.causal ? min(tiles, (q0 + 32 * NQ + CHA - 1) / CHA) : tiles;
+  const int whole = min(mine, (a.causal ? min(n, q0 + 1) : n) / CHA);
+  int t = 0;
+  for (; t < whole; ++t) { arrive(t); compute(t, std::false_type{}); }
+  for (; t < mine; ++t) { arrive(t); compute(t, std::true_type{}); }
+  for (; t < tiles; ++t) arrive(t);
   __syncthreads();   // the images are no longer read: a quarter of them is each wave's way out
   if (!active) return;
   const float kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
@@ -233,14 +270,12 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int q0 = base_q + wave * 32, q = q0 + (lane & 31);
   const bool active = q0 < n;
-  const E* kb_ = (const E*)a.k + sq.first * a.ldk + (long long)hk * a.d;
-  const E* vb_ = (const E*)a.v + sq.first * a.ldv + (long long)hk * a.d;
+  const Tiles<E, DP> kt(a.k, sq.first, a.ldk, hk, n, a.d, wave, lane), vt(a.v, sq.first, a.ldv, hk, n, a.d, wave, lane);
   const int last = a.causal ? min(n, base_q + 128) : n, tiles = (last + CHA - 1) / CHA;
   const auto fetch = [&](int t) {
     char* dst = lds + (t & 1) * 2 * I::IMG;
-    const int rows = min(CHA, n - t * CHA);
-    I::load(kb_ + (long long)t * CHA * a.ldk, (uint32_t)a.ldk, rows, a.d, dst, wave, lane);
-    I::load(vb_ + (long long)t * CHA * a.ldv, (uint32_t)a.ldv, rows, a.d, dst + I::IMG, wave, lane);
+    kt.fetch(t * CHA, dst, wave);
+    vt.fetch(t * CHA, dst + I::IMG, wave);
   };
   fetch(0);
   bf16x8 qf[DP / 16], gf[DP / 16];
@@ -260,12 +295,12 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
         for (int i = 0; i < 8; ++i) D = fmaf(to_f32(gv[i]), to_f32(ov[i]), D);
       }
     }
-    nl = -a.lse[(long long)h * a.rows + sq.first + q] * LOG2E;
+    nl = -a.lse[(long long)h * a.rows + sq.first + q] / a.scale;
   }
   D = half_sum(D);
   if (q < n && lane < 32) {
     a.nlse2[(long long)h * a.rows + sq.first + q] = nl;
-    a.delta[(long long)h * a.rows + sq.first + q] = D;
+    a.delta[(long long)h * a.rows + sq.first + q] = -D;
   }
   f32x16 dq[DP / 32];
 #pragma unroll
@@ -273,27 +308,28 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
   const float c = a.scale * LOG2E, kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
   DropKey key;
   if (DROP) key = drop_key(a.seed, a.site, a.step);
-  for (int t = 0; t < tiles; ++t) {
+  const auto arrive = [&](int t) {
     wait_vm0();
     __syncthreads();
     if (t + 1 < tiles) fetch(t + 1);
+  };
+  const auto compute = [&](int t, auto edge) {
     const int k0 = t * CHA;
-    if (!active || (a.causal && k0 >= q0 + 32)) continue;
     const char* Ks = lds + (t & 1) * 2 * I::IMG;
     const char* Vs = Ks + I::IMG;
-    const bool edge = k0 + CHA > n || (a.causal && k0 + CHA - 1 > q0);
     const int lim = (a.causal ? min(n, q + 1) : n) - k0 - 4 * (lane >> 5);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      f32x16 s = zero16(), g = zero16();
+      // the accumulators start from -lse / scale and -D instead of zero, which leaves one product each for P and dS
+      f32x16 s = splat16(nl), g = splat16(DROP ? 0.f : -D);
 #pragma unroll
       for (int st = 0; st < DP / 16; ++st) {
         s = mfma_32x32x16<E>(I::rows_frag(Ks, kb * 32 + (lane & 31), st, lane), qf[st], s);
         g = mfma_32x32x16<E>(I::rows_frag(Vs, kb * 32 + (lane & 31), st, lane), gf[st], g);
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, nl));
-      if (edge) {
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * c);
+      if constexpr (decltype(edge)::value) {
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (kb * 32 + 8 * (r >> 2) + (r & 3) >= lim) s[r] = 0.f;
@@ -304,7 +340,7 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
         for (int r = 0; r < 16; ++r) g[r] = s[r] * (drop_keeps(bytes, r, a.drop) ? fmaf(g[r], kept, -D) : -D);
       } else {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) g[r] = s[r] * (g[r] - D);
+        for (int r = 0; r < 16; ++r) g[r] *= s[r];
       }
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
@@ -312,8 +348,15 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
 #pragma unroll
         for (int t2 = 0; t2 < DP / 32; ++t2) dq[t2] = mfma_32x32x16<E>(I::rows_T(Ks, kb, s2, t2, lane), df, dq[t2]);
       }
+      if (DP > 64) __builtin_amdgcn_sched_barrier(0);   // (the halves side by side want more registers than two waves a SIMD have)
     }
-  }
+  };
+  const int mine = !active ? 0 : a.causal ? min(tiles, (q0 + 32 + CHA - 1) / CHA) : tiles;   // (as in the forward kernel)
+  const int whole = min(mine, (a.causal ? min(n, q0 + 1) : n) / CHA);
+  int t = 0;
+  for (; t < whole; ++t) { arrive(t); compute(t, std::false_type{}); }
+  for (; t < mine; ++t) { arrive(t); compute(t, std::true_type{}); }
+  for (; t < tiles; ++t) arrive(t);
   __syncthreads();
   if (!active) return;
   store_rows<E, DP>(dq, lds + wave * I::IMG, (E*)a.dq + (sq.first + q0) * a.lddq + (long long)h * a.d, a.lddq, n - q0, a.d, lane, a.scale);
@@ -340,16 +383,21 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   const bool active = key0 < n;
   // query tiles of one head: with a causal mask from the one that holds this block's first key on
   const int t0 = a.causal ? base_k / CHA : 0, per_head = (n + CHA - 1) / CHA - t0, tiles = per_head * group;
+  Tiles<E, DP> qt(a.q, sq.first, a.ldq, hk * group, n, a.d, wave, lane), gt(a.dout, sq.first, a.lddo, hk * group, n, a.d, wave, lane);
+  const float* stats = (wave ? a.delta : a.nlse2) + (long long)hk * group * a.rows + sq.first;
+  int next_t = t0;   // the next tile to be fetched, of the head that the three point at
   const auto fetch = [&](int i) {
     char* dst = lds + (i & 1) * STAGE;
-    const int h = hk * group + i / per_head, row0 = (t0 + i % per_head) * CHA, rows = min(CHA, n - row0);
-    const long long tok = sq.first + row0;
-    I::load((const E*)a.q + tok * a.ldq + (long long)h * a.d, (uint32_t)a.ldq, rows, a.d, dst, wave, lane);
-    I::load((const E*)a.dout + tok * a.lddo + (long long)h * a.d, (uint32_t)a.lddo, rows, a.d, dst + I::IMG, wave, lane);
-    if (wave < 2) {   // rows past the sequence: zeros, which add nothing (their Q and dO are zeros too)
-      const float* src = (wave ? a.delta : a.nlse2) + (long long)h * a.rows + tok;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(src, (uint32_t)rows * 4), (__attribute__((address_space(3))) void*)(dst + 2 * I::IMG + wave * 256),
-                                               4, lane * 4, 0, 0, 0);
+    qt.fetch(next_t * CHA, dst, wave);
+    gt.fetch(next_t * CHA, dst + I::IMG, wave);
+    if (wave < 2)   // rows past the sequence: zeros, which add nothing (their Q and dO are zeros too)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(stats + next_t * CHA, (uint32_t)min(CHA, n - next_t * CHA) * 4),
+                                               (__attribute__((address_space(3))) void*)(dst + 2 * I::IMG + wave * 256), 4, lane * 4, 0, 0, 0);
+    if (++next_t == t0 + per_head) {
+      next_t = t0;
+      qt.base += a.d;
+      gt.base += a.d;
+      stats += a.rows;
     }
   };
   fetch(0);
@@ -362,46 +410,56 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   const float c = a.scale * LOG2E, kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
   DropKey key;
   if (DROP) key = drop_key(a.seed, a.site, a.step);
-  for (int i = 0; i < tiles; ++i) {
+  int i = 0;   // tiles so far, of all heads
+  const auto arrive = [&] {
     wait_vm0();
     __syncthreads();
     if (i + 1 < tiles) fetch(i + 1);
-    const int h = hk * group + i / per_head, row0 = (t0 + i % per_head) * CHA;
-    if (!active || (a.causal && row0 + CHA <= key0)) continue;
+  };
+  const auto compute = [&](int h, int row0, auto edge) {
     const char* Qs = lds + (i & 1) * STAGE;
     const char* Gs = Qs + I::IMG;
     const float* Ls = (const float*)(Gs + I::IMG);
     const float* Ds = Ls + 64;
-    const bool edge = a.causal && row0 < key0 + 31;
     const int lim = kk - row0 - 4 * (lane >> 5);   // causal: rows below it do not see this lane's key
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
-      f32x16 s = zero16(), g = zero16();
-#pragma unroll
-      for (int st = 0; st < DP / 16; ++st) {
-        s = mfma_32x32x16<E>(I::rows_frag(Qs, qb * 32 + (lane & 31), st, lane), kf[st], s);
-        g = mfma_32x32x16<E>(I::rows_frag(Gs, qb * 32 + (lane & 31), st, lane), vf[st], g);
-      }
-      u32x4 bytes;
-      if (DROP) bytes = drop_bytes<false>(row0 + qb * 32, key0, (uint32_t)(b * a.heads + h), key, lane);
+      f32x16 s, g;   // (from -lse / scale and -D, as in the dQ kernel)
 #pragma unroll
       for (int blk4 = 0; blk4 < 4; ++blk4) {
         const f32x4 L4 = *(const f32x4*)(Ls + qb * 32 + 8 * blk4 + 4 * (lane >> 5));
         const f32x4 D4 = *(const f32x4*)(Ds + qb * 32 + 8 * blk4 + 4 * (lane >> 5));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int r = 4 * blk4 + j;
-          float p = __builtin_amdgcn_exp2f(fmaf(s[r], c, L4[j]));
-          if (edge) p = qb * 32 + 8 * blk4 + j < lim ? 0.f : p;
-          if (DROP) {
+        for (int j = 0; j < 4; ++j) { s[4 * blk4 + j] = L4[j]; g[4 * blk4 + j] = DROP ? 0.f : D4[j]; }
+      }
+#pragma unroll
+      for (int st = 0; st < DP / 16; ++st) {
+        s = mfma_32x32x16<E>(I::rows_frag(Qs, qb * 32 + (lane & 31), st, lane), kf[st], s);
+        g = mfma_32x32x16<E>(I::rows_frag(Gs, qb * 32 + (lane & 31), st, lane), vf[st], g);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * c);
+      if constexpr (decltype(edge)::value) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (qb * 32 + 8 * (r >> 2) + (r & 3) < lim) s[r] = 0.f;
+      }
+      if (DROP) {
+        const u32x4 bytes = drop_bytes<false>(row0 + qb * 32, key0, (uint32_t)(b * a.heads + h), key, lane);
+#pragma unroll
+        for (int blk4 = 0; blk4 < 4; ++blk4) {
+          const f32x4 D4 = *(const f32x4*)(Ds + qb * 32 + 8 * blk4 + 4 * (lane >> 5));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int r = 4 * blk4 + j;
             const bool keep = drop_keeps(bytes, r, a.drop);
-            g[r] = p * (keep ? fmaf(g[r], kept, -D4[j]) : -D4[j]);
-            s[r] = keep ? p : 0.f;
-          } else {
-            g[r] = p * (g[r] - D4[j]);
-            s[r] = p;
+            g[r] = s[r] * (keep ? fmaf(g[r], kept, D4[j]) : D4[j]);
+            s[r] = keep ? s[r] : 0.f;
           }
         }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) g[r] *= s[r];
       }
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
@@ -413,6 +471,15 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
         }
       }
     }
+  };
+  // per head: tiles before the wave's first key, where it only helps to load, those with a mask, those whole
+  const int idle = !active ? per_head : a.causal ? min(per_head, key0 / CHA - t0) : 0;
+  const int masked = a.causal ? min(per_head, (key0 + 31 + CHA - 1) / CHA - t0) : 0;
+  for (int h = hk * group; h < (hk + 1) * group; ++h) {
+    int t = 0;
+    for (; t < idle; ++t, ++i) arrive();
+    for (; t < masked; ++t, ++i) { arrive(); compute(h, (t0 + t) * CHA, std::true_type{}); }
+    for (; t < per_head; ++t, ++i) { arrive(); compute(h, (t0 + t) * CHA, std::false_type{}); }
   }
   __syncthreads();
   if (!active) return;
