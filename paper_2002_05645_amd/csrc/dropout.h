@@ -24,12 +24,14 @@ __device__ __forceinline__ DropKey drop_key(uint64_t seed, uint64_t site, const 
   return DropKey{(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)site, (uint32_t)(site >> 32)};
 }
 
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }   // one instruction
+
 __device__ __forceinline__ u32x4 philox7(uint32_t c0, uint32_t c1, const DropKey& key) {
   uint32_t c2 = key.s0, c3 = key.s1, k0 = key.k0, k1 = key.k1;
 #pragma unroll
   for (int r = 0; r < 7; ++r) {
     const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-    const uint32_t n0 = (uint32_t)(b >> 32) ^ c1 ^ k0, n2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    const uint32_t n0 = xor3((uint32_t)(b >> 32), c1, k0), n2 = xor3((uint32_t)(a >> 32), c3, k1);
     c0 = n0; c1 = (uint32_t)b; c2 = n2; c3 = (uint32_t)a;
     k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
   }
@@ -70,6 +72,12 @@ __device__ __forceinline__ u32x4 drop_bytes(int i0, int j0, uint32_t pair, const
   const uint32_t I = (uint32_t)i0 / 4 + (QL ? along : across), J = (uint32_t)j0 / 4 + (QL ? across : along);
   const u32x4 w = philox7(I << 16 | J, 0x80000000u | pair, key);
   return quad_transpose(QL ? w : byte_transpose(w), lane);
+}
+// keeps ? x : 0, done here and in 32 bits: left to itself the compiler makes the choice behind the rounding to 16 bits, value by value
+__device__ __forceinline__ float drop_select(bool keeps, float x) {
+  x = keeps ? x : 0.f;
+  asm("" : "+v"(x));
+  return x;
 }
 __device__ __forceinline__ bool drop_keeps(const u32x4& bytes, int r, uint32_t drop) {
   return ((bytes[r >> 2] >> (8 * (r & 3))) & 255u) >= drop;

@@ -2372,6 +2372,7 @@ static SeqAttnArgs attention_args(l2l_ctx* c, const l2l_attention* a, const void
   g.rows = a->rows; g.scale = a->scale;
   (void)drop_threshold(a->dropout, 256, &g.drop);
   g.seed = a->seed; g.site = a->site; g.step = a->step;
+  g.by_xcd = 2LL * a->max_len * a->head_dim * (long long)esize(a->dtype) >= 2 << 20;   // (half of an XCD's L2)
   g.bad = c->bad_ids;
   return g;
 }

@@ -19,6 +19,7 @@ struct SeqAttnArgs {
   uint32_t drop;                      // of 256; 0 = no dropout
   uint64_t seed, site;
   const uint64_t* step;
+  int by_xcd;                         // 1: whole (sequence, key head) units to an XCD
   int32_t* bad;                       // bit 1: a sequence did not fit rows or max_len
 };
 

@@ -81,11 +81,10 @@ __global__ __launch_bounds__(256) void seq_fwd_f32_kernel(const SeqAttnArgs a) {
   using I = ImgF<DP>;
   __shared__ __attribute__((aligned(16))) float lds[2 * I::FLOATS];
   float *Ks = lds, *Vs = lds + I::FLOATS;
-  const int nblk = (a.max_len + 127) / 128;
-  const long long id = xcd_order();
-  if (id >= (long long)a.sequences * a.heads * nblk) return;
-  const int blk = nblk - 1 - (int)(id % nblk);
-  const int bh = (int)(id / nblk), b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv_heads);
+  const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
+  const Place at = place(a, group * nblk);
+  const int blk = nblk - 1 - at.block % nblk;
+  const int b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads, h = hk * group + at.block / nblk, bh = b * a.heads + h;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_q = blk * 128;
   if (base_q >= n) return;
@@ -161,11 +160,10 @@ __global__ __launch_bounds__(256) void seq_bwd_dq_f32_kernel(const SeqAttnArgs a
   using I = ImgF<DP>;
   __shared__ __attribute__((aligned(16))) float lds[2 * I::FLOATS];
   float *Ks = lds, *Vs = lds + I::FLOATS;
-  const int nblk = (a.max_len + 127) / 128;
-  const long long id = xcd_order();
-  if (id >= (long long)a.sequences * a.heads * nblk) return;
-  const int blk = nblk - 1 - (int)(id % nblk);
-  const int bh = (int)(id / nblk), b = bh / a.heads, h = bh % a.heads, hk = h / (a.heads / a.kv_heads);
+  const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
+  const Place at = place(a, group * nblk);
+  const int blk = nblk - 1 - at.block % nblk;
+  const int b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads, h = hk * group + at.block / nblk, bh = b * a.heads + h;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_q = blk * 128;
   if (base_q >= n) return;
@@ -237,11 +235,9 @@ __global__ __launch_bounds__(256) void seq_bwd_dkv_f32_kernel(const SeqAttnArgs 
   using I = ImgF<DP>;
   __shared__ __attribute__((aligned(16))) float lds[2 * I::FLOATS + 64];
   float *Qs = lds, *Gs = lds + I::FLOATS, *Ls = lds + 2 * I::FLOATS, *Ds = Ls + 32;
-  const int nblk = (a.max_len + 127) / 128;
-  const long long id = xcd_order();
-  if (id >= (long long)a.sequences * a.kv_heads * nblk) return;
-  const int blk = (int)(id % nblk);
-  const int bk = (int)(id / nblk), b = bk / a.kv_heads, hk = bk % a.kv_heads, group = a.heads / a.kv_heads;
+  const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
+  const Place at = place(a, nblk);
+  const int blk = at.block, b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_k = blk * 128;
   if (base_k >= n) return;

@@ -21,10 +21,9 @@ typedef fp16 Elem;
 
 namespace {
 
-// one workgroup per `rows_per` rows of every (sequence, head), rounded up to a multiple of the 8 XCDs
+// one workgroup per `rows_per` rows of every (sequence, head)
 dim3 blocks(const SeqAttnArgs& a, int heads, int rows_per) {
-  const long long n = (long long)a.sequences * heads * ((a.max_len + rows_per - 1) / rows_per);
-  return dim3((unsigned)((n + 7) / 8 * 8));
+  return dim3((unsigned)((long long)a.sequences * heads * ((a.max_len + rows_per - 1) / rows_per)));
 }
 
 template <typename K>
