@@ -90,6 +90,25 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[DP / 32], char* s
   }
 }
 
+// Loads from memory straight into LDS (lane l's 16 or 4 bytes to `dst` + 16 l or 4 l), which have no register to be waited for: the
+// waits are the kernels' own (wait_vm0 at the head of a tile).  As built-ins, the compiler counts them before every transposing LDS read,
+// whose place it does not know, and so takes the next tile's loads for this tile's.  The no-op is the wait state between M0 and
+// its use.
+__device__ __forceinline__ i32x4 lds_source(const void* base, uint32_t bytes) {
+  const uint64_t p = (uint64_t)base;
+  return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)p), __builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)) & 0xFFFF,
+               __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
+}
+__device__ __forceinline__ uint32_t lds_place(const char* dst) {
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)dst);
+}
+__device__ __forceinline__ void lds_load16(i32x4 from, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void lds_load4(i32x4 from, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(from) : "memory", "m0");
+}
+
 // 64 rows of a matrix into an LDS image, 16 bytes a lane and instruction, by the four waves of a workgroup: the lanes' places within a tile
 // are worked out once, a tile moves only the descriptor.  Rows past the sequence and columns past the head lie outside the descriptor
 // and arrive as zeros.
@@ -110,10 +129,10 @@ struct Tiles {
     }
   }
   __device__ __forceinline__ void fetch(int row0, char* dst, int wave) const {
-    const __amdgpu_buffer_rsrc_t rs = make_rsrc(base + (long long)row0 * ld, (uint32_t)(((long long)(min(CHA, n - row0) - 1) * ld + d) * 2));
+    const i32x4 from = lds_source(base + (long long)row0 * ld, (uint32_t)(((long long)(min(CHA, n - row0) - 1) * ld + d) * 2));
+    const uint32_t to = lds_place(dst) + wave * 1024;
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(dst + (i * 4 + wave) * 1024), 16, (int)off[i], 0, 0, 0);
+    for (int i = 0; i < PER; ++i) lds_load16(from, off[i], to + i * 4096);
   }
 };
 __device__ __forceinline__ f32x16 splat16(float x) { return f32x16{x, x, x, x, x, x, x, x, x, x, x, x, x, x, x, x}; }
@@ -122,7 +141,7 @@ __device__ __forceinline__ f32x16 splat16(float x) { return f32x16{x, x, x, x, x
 // A workgroup owns 128 NQ queries of one (sequence, head), each of its four waves 32 NQ of them, and walks the keys in tiles of 64; the next
 // tile's K and V are on their way into the other half of the LDS while one is computed.
 template <typename E, int DP, int NQ, bool DROP>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 64 && NQ == 1 ? (DROP ? 3 : 4) : 2)))
 void seq_fwd_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
   __shared__ __attribute__((aligned(1024))) char lds[4 * I::IMG];
@@ -357,7 +376,7 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
 #pragma unroll
         for (int t2 = 0; t2 < DP / 32; ++t2) dq[t2] = mfma_32x32x16<E>(I::rows_T(Ks, kb, s2, t2, lane), df, dq[t2]);
       }
-      if (DP > 64) __builtin_amdgcn_sched_barrier(0);   // (the halves side by side want more registers than two waves a SIMD have)
+      __builtin_amdgcn_sched_barrier(0);   // (the halves side by side want more registers than the waves of a SIMD have)
     }
   };
   const int mine = !active ? 0 : a.causal ? min(tiles, (q0 + 32 + CHA - 1) / CHA) : tiles;   // (as in the forward kernel)
@@ -398,8 +417,7 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
     qt.fetch(next_t * CHA, dst, wave);
     gt.fetch(next_t * CHA, dst + I::IMG, wave);
     if (wave < 2)   // rows past the sequence: zeros, which add nothing (their Q and dO are zeros too)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(stats + next_t * CHA, (uint32_t)min(CHA, n - next_t * CHA) * 4),
-                                               (__attribute__((address_space(3))) void*)(dst + 2 * I::IMG + wave * 256), 4, lane * 4, 0, 0, 0);
+      lds_load4(lds_source(stats + next_t * CHA, (uint32_t)min(CHA, n - next_t * CHA) * 4), lane * 4, lds_place(dst) + 2 * I::IMG + wave * 256);
     if (++next_t == t0 + per_head) {
       next_t = t0;
       qt.base += a.d;
