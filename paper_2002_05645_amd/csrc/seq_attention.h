@@ -56,9 +56,10 @@ __device__ __forceinline__ Place place(const SeqAttnArgs& a, int per_unit) {
 struct Seq { long long first; int n; };
 // rows of sequence b; n = 0 for one that does not fit the rows or the longest length (reported, not followed)
 __device__ __forceinline__ Seq sequence(const SeqAttnArgs& a, int b) {
+  typedef const __attribute__((address_space(4))) int32_t* Scalar;   // (through the scalar cache, which other workgroups have filled)
   Seq s;
-  s.first = a.first ? (long long)a.first[b] : (long long)b * a.max_len;
-  s.n = a.len ? a.len[b] : a.max_len;
+  s.first = a.first ? (long long)((Scalar)(uintptr_t)a.first)[b] : (long long)b * a.max_len;
+  s.n = a.len ? ((Scalar)(uintptr_t)a.len)[b] : a.max_len;
   if (s.n < 0 || s.n > a.max_len || s.first < 0 || s.first + s.n > a.rows) {
     if (threadIdx.x == 0 && s.n != 0) atomicOr(a.bad, 2);
     s.n = 0;
@@ -93,20 +94,18 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[DP / 32], char* s
 // Loads from memory straight into LDS (lane l's 16 or 4 bytes to `dst` + 16 l or 4 l), which have no register to be waited for: the
 // waits are the kernels' own (wait_vm0 at the head of a tile).  As built-ins, the compiler counts them before every transposing LDS read,
 // whose place it does not know, and so takes the next tile's loads for this tile's.  The no-op is the wait state between M0 and
-// its use.
+// its use; nothing else in these kernels uses M0.
 __device__ __forceinline__ i32x4 lds_source(const void* base, uint32_t bytes) {
   const uint64_t p = (uint64_t)base;
   return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)p), __builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)) & 0xFFFF,
                __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
 }
-__device__ __forceinline__ uint32_t lds_place(const char* dst) {
-  return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)dst);
-}
+__device__ __forceinline__ uint32_t lds_place(const __attribute__((address_space(3))) char* p) { return (uint32_t)(uintptr_t)p; }
 __device__ __forceinline__ void lds_load16(i32x4 from, uint32_t off, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(from) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(off), "s"(from) : "memory");
 }
 __device__ __forceinline__ void lds_load4(i32x4 from, uint32_t off, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(from) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(off), "s"(from) : "memory");
 }
 
 // 64 rows of a matrix into an LDS image, 16 bytes a lane and instruction, by the four waves of a workgroup: the lanes' places within a tile
@@ -128,11 +127,11 @@ struct Tiles {
       off[i] = c * 8 < d ? ((uint32_t)row * (uint32_t)ld + (uint32_t)c * 8) * 2u : BUF_OOB;
     }
   }
-  __device__ __forceinline__ void fetch(int row0, char* dst, int wave) const {
+  // to: the image's place in LDS
+  __device__ __forceinline__ void fetch(int row0, uint32_t to, int wave) const {
     const i32x4 from = lds_source(base + (long long)row0 * ld, (uint32_t)(((long long)(min(CHA, n - row0) - 1) * ld + d) * 2));
-    const uint32_t to = lds_place(dst) + wave * 1024;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) lds_load16(from, off[i], to + i * 4096);
+    for (int i = 0; i < PER; ++i) lds_load16(from, off[i], to + wave * 1024 + i * 4096);
   }
 };
 __device__ __forceinline__ f32x16 splat16(float x) { return f32x16{x, x, x, x, x, x, x, x, x, x, x, x, x, x, x, x}; }
@@ -157,10 +156,11 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
   const bool active = q0 < n;   // (per wave)
   const Tiles<E, DP> kt(a.k, sq.first, a.ldk, hk, n, a.d, wave, lane), vt(a.v, sq.first, a.ldv, hk, n, a.d, wave, lane);
   const int last = a.causal ? min(n, base_q + 128 * NQ) : n, tiles = (last + CHA - 1) / CHA;
+  const uint32_t lds0 = lds_place((const __attribute__((address_space(3))) char*)lds);
   const auto fetch = [&](int t) {
-    char* dst = lds + (t & 1) * 2 * I::IMG;
-    kt.fetch(t * CHA, dst, wave);
-    vt.fetch(t * CHA, dst + I::IMG, wave);
+    const uint32_t to = lds0 + (t & 1) * 2 * I::IMG;
+    kt.fetch(t * CHA, to, wave);
+    vt.fetch(t * CHA, to + I::IMG, wave);
   };
   fetch(0);
   bf16x8 qf[NQ][DP / 16];
@@ -300,10 +300,11 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
   const bool active = q0 < n;
   const Tiles<E, DP> kt(a.k, sq.first, a.ldk, hk, n, a.d, wave, lane), vt(a.v, sq.first, a.ldv, hk, n, a.d, wave, lane);
   const int last = a.causal ? min(n, base_q + 128) : n, tiles = (last + CHA - 1) / CHA;
+  const uint32_t lds0 = lds_place((const __attribute__((address_space(3))) char*)lds);
   const auto fetch = [&](int t) {
-    char* dst = lds + (t & 1) * 2 * I::IMG;
-    kt.fetch(t * CHA, dst, wave);
-    vt.fetch(t * CHA, dst + I::IMG, wave);
+    const uint32_t to = lds0 + (t & 1) * 2 * I::IMG;
+    kt.fetch(t * CHA, to, wave);
+    vt.fetch(t * CHA, to + I::IMG, wave);
   };
   fetch(0);
   bf16x8 qf[DP / 16], gf[DP / 16];
@@ -392,12 +393,17 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
 
 // ---- dK, dV -----------------------------------------------------------------------------------------------------------
 // A workgroup owns 128 keys of one (sequence, key head) and walks the queries of all the head's query heads in tiles of 64.
-template <typename E, int DP, bool DROP>
+// WHOLE, where no sequence is longer than 128: the workgroup has all keys of its head, so that dQ of a tile can be made here as well, from dS
+// that the waves lay side by side in LDS, and the dQ kernel with its second pass over scores, probabilities and masks is not run.  The
+// rows' D and lse are taken from O, dO and lse at the head's start.
+template <typename E, int DP, bool DROP, bool WHOLE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP > 96 ? 1 : 2)))
 void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
+  using IS = Any<64>;                       // dS: [key][64 queries]
   constexpr int STAGE = 2 * I::IMG + 512;   // Q, dO, and 64 rows' -lse and D
-  __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
+  constexpr int KIMG = 2 * STAGE, SIMG = KIMG + 2 * I::IMG, STAT = SIMG + 2 * IS::IMG;   // (WHOLE) K, dS, two heads' -lse and D of 128 rows
+  __shared__ __attribute__((aligned(1024))) char lds[WHOLE ? STAT + 2 * 1024 : 2 * STAGE];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
   const Place at = place(a, nblk);
   const int blk = at.block, b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads;
@@ -412,12 +418,13 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   Tiles<E, DP> qt(a.q, sq.first, a.ldq, hk * group, n, a.d, wave, lane), gt(a.dout, sq.first, a.lddo, hk * group, n, a.d, wave, lane);
   const float* stats = (wave ? a.delta : a.nlse2) + (long long)hk * group * a.rows + sq.first;
   int next_t = t0;   // the next tile to be fetched, of the head that the three point at
+  const uint32_t lds0 = lds_place((const __attribute__((address_space(3))) char*)lds);
   const auto fetch = [&](int i) {
-    char* dst = lds + (i & 1) * STAGE;
-    qt.fetch(next_t * CHA, dst, wave);
-    gt.fetch(next_t * CHA, dst + I::IMG, wave);
-    if (wave < 2)   // rows past the sequence: zeros, which add nothing (their Q and dO are zeros too)
-      lds_load4(lds_source(stats + next_t * CHA, (uint32_t)min(CHA, n - next_t * CHA) * 4), lane * 4, lds_place(dst) + 2 * I::IMG + wave * 256);
+    const uint32_t to = lds0 + (i & 1) * STAGE;
+    qt.fetch(next_t * CHA, to, wave);
+    gt.fetch(next_t * CHA, to + I::IMG, wave);
+    if (!WHOLE && wave < 2)   // rows past the sequence: zeros, which add nothing (their Q and dO are zeros too)
+      lds_load4(lds_source(stats + next_t * CHA, (uint32_t)min(CHA, n - next_t * CHA) * 4), lane * 4, to + 2 * I::IMG + wave * 256);
     if (++next_t == t0 + per_head) {
       next_t = t0;
       qt.base += a.d;
@@ -426,6 +433,33 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
     }
   };
   fetch(0);
+  if constexpr (WHOLE) {
+    const Tiles<E, DP> kt(a.k, sq.first, a.ldk, hk, n, a.d, wave, lane);
+    kt.fetch(0, lds0 + KIMG, wave);
+    if (n > CHA) kt.fetch(CHA, lds0 + KIMG + I::IMG, wave);
+  }
+  // WHOLE: -lse / scale and -D of the head's rows, two threads to a row (zeros past the sequence)
+  const auto head_stats = [&](int h) {
+    const int row = threadIdx.x >> 1, half = threadIdx.x & 1;
+    float D = 0.f, nl = 0.f;
+    if (row < n) {
+      const E* grow = (const E*)a.dout + (sq.first + row) * a.lddo + (long long)h * a.d;
+      const E* orow = (const E*)a.o + (sq.first + row) * a.ldo + (long long)h * a.d;
+#pragma unroll
+      for (int u = 0; u < DP / 16; ++u) {
+        const int col = (2 * u + half) * 8;
+        if (col < a.d) {
+          const typename Vec<E>::x8 gv = *(const typename Vec<E>::x8*)(grow + col), ov = *(const typename Vec<E>::x8*)(orow + col);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) D = fmaf(to_f32(gv[j]), to_f32(ov[j]), D);
+        }
+      }
+      nl = -a.lse[(long long)h * a.rows + sq.first + row] / a.scale;
+    }
+    D += dpp_move<0xB1>(D);   // the neighbour's half
+    float* st = (float*)(lds + STAT + (h & 1) * 1024);
+    st[half * 128 + row] = half ? -D : nl;
+  };
   bf16x8 kf[DP / 16], vf[DP / 16];
   I::template row_frags<E>((const E*)a.k + (sq.first + kk) * a.ldk + (long long)hk * a.d, kk < n, a.d, lane, kf);
   I::template row_frags<E>((const E*)a.v + (sq.first + kk) * a.ldv + (long long)hk * a.d, kk < n, a.d, lane, vf);
@@ -444,8 +478,8 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   const auto compute = [&](int h, int row0, auto edge) {
     const char* Qs = lds + (i & 1) * STAGE;
     const char* Gs = Qs + I::IMG;
-    const float* Ls = (const float*)(Gs + I::IMG);
-    const float* Ds = Ls + 64;
+    const float* Ls = WHOLE ? (const float*)(lds + STAT + (h & 1) * 1024) + row0 : (const float*)(Gs + I::IMG);
+    const float* Ds = Ls + (WHOLE ? 128 : 64);
     const int lim = kk - row0 - 4 * (lane >> 5);   // causal: rows below it do not see this lane's key
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
@@ -486,6 +520,10 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) g[r] *= s[r];
       }
+      if (WHOLE && key0 + 32 > n) {   // a key past the sequence has a row of K that is zero, and a dS that may be anything
+#pragma unroll
+        for (int r = 0; r < 16; ++r) g[r] = kk < n ? g[r] : 0.f;
+      }
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
         const bf16x8 pf = pack8<E>(s, 8 * s2), df = pack8<E>(g, 8 * s2);
@@ -493,6 +531,44 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
         for (int t2 = 0; t2 < DP / 32; ++t2) {
           dv[t2] = mfma_32x32x16<E>(I::rows_T(Gs, qb, s2, t2, lane), pf, dv[t2]);
           dk[t2] = mfma_32x32x16<E>(I::rows_T(Qs, qb, s2, t2, lane), df, dk[t2]);
+        }
+        if constexpr (WHOLE) {   // registers 8 s2 .. of this key's row: queries 16 s2 + 8 {0, 1} + 4 (lane / 32) + 0..3
+          const int row = key0 + (lane & 31);
+          const u32x4 w = __builtin_bit_cast(u32x4, df);
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            *(u32x2*)(lds + SIMG + row * IS::PITCH + IS::slot(row & 63, qb * 4 + 2 * s2 + x) * 16 + 8 * (lane >> 5)) = x ? u32x2{w.z, w.w} : u32x2{w.x, w.y};
+        }
+      }
+      if (WHOLE) __builtin_amdgcn_sched_barrier(0);   // (the halves side by side want more registers than two waves a SIMD have)
+    }
+  };
+  // WHOLE: dQ^T = K^T dS^T of the tile, a 32 x 32 block of (columns, queries) to a wave at a time
+  const auto query_grads = [&](int h, int row0) {
+    __syncthreads();   // every wave's dS is in
+    const int nkb = min((n + 31) / 32, a.causal ? (row0 + CHA) / 32 : 4);   // (the keys behind have no weight and no dS)
+#pragma unroll
+    for (int j = 0; j < (2 * (DP / 32) + 3) / 4; ++j) {
+      const int idx = wave + 4 * j, qb = idx & 1, t2 = idx >> 1, q = row0 + qb * 32 + (lane & 31);
+      if (t2 >= DP / 32) break;
+      f32x16 dq = zero16();
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+        if (kb < nkb) {
+#pragma unroll
+          for (int s2 = 0; s2 < 2; ++s2)
+            dq = mfma_32x32x16<E>(I::rows_T(lds + KIMG + (kb >> 1) * I::IMG, kb & 1, s2, t2, lane),
+                                  IS::rows_T(lds + SIMG + (kb >> 1) * IS::IMG, kb & 1, s2, qb, lane), dq);
+        }
+      if (q < n) {
+        E* out = (E*)a.dq + (sq.first + q) * a.lddq + (long long)h * a.d;
+#pragma unroll
+        for (int blk4 = 0; blk4 < 4; ++blk4) {
+          const int col = t2 * 32 + blk4 * 8 + 4 * (lane >> 5);
+          typename Vec<E>::x4 v;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] = from_f32<E>(dq[blk4 * 4 + x] * a.scale);
+          if (col < a.d) *(typename Vec<E>::x4*)(out + col) = v;
         }
       }
     }
@@ -502,9 +578,13 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   const int masked = a.causal ? min(per_head, (key0 + 31 + CHA - 1) / CHA - t0) : 0;
   for (int h = hk * group; h < (hk + 1) * group; ++h) {
     int t = 0;
-    for (; t < idle; ++t, ++i) arrive();
-    for (; t < masked; ++t, ++i) { arrive(); compute(h, (t0 + t) * CHA, std::true_type{}); }
-    for (; t < per_head; ++t, ++i) { arrive(); compute(h, (t0 + t) * CHA, std::false_type{}); }
+    if (WHOLE) head_stats(h);
+    const auto grads = [&] {
+      if constexpr (WHOLE) query_grads(h, (t0 + t) * CHA);
+    };
+    for (; t < idle; ++t, ++i) { arrive(); grads(); }
+    for (; t < masked; ++t, ++i) { arrive(); compute(h, (t0 + t) * CHA, std::true_type{}); grads(); }
+    for (; t < per_head; ++t, ++i) { arrive(); compute(h, (t0 + t) * CHA, std::false_type{}); grads(); }
   }
   __syncthreads();
   if (!active) return;

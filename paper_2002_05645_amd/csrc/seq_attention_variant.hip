@@ -51,12 +51,20 @@ void L2L_NAME(l2l_seq_attn_bwd_)(const SeqAttnArgs& a, hipStream_t s) {
     go(sattn::seq_bwd_dkv_f32_kernel<L2L_DP, false>, blocks(a, a.kv_heads, 128), a, s);
   }
 #else
-  if (a.drop) {
-    go(sattn::seq_bwd_dq_kernel<Elem, L2L_DP, true>, blocks(a, a.heads, 128), a, s);
-    go(sattn::seq_bwd_dkv_kernel<Elem, L2L_DP, true>, blocks(a, a.kv_heads, 128), a, s);
-  } else {
-    go(sattn::seq_bwd_dq_kernel<Elem, L2L_DP, false>, blocks(a, a.heads, 128), a, s);
-    go(sattn::seq_bwd_dkv_kernel<Elem, L2L_DP, false>, blocks(a, a.kv_heads, 128), a, s);
-  }
+  const auto both = [&](auto drop) {
+    constexpr bool D = decltype(drop)::value;
+    if constexpr (L2L_DP <= 64) {   // (wider heads leave no registers for it)
+      if (a.max_len <= 128) {       // a workgroup has all of a head's keys: one kernel does both
+        go(sattn::seq_bwd_dkv_kernel<Elem, L2L_DP, D, true>, blocks(a, a.kv_heads, 128), a, s);
+        return;
+      }
+    }
+    {
+      go(sattn::seq_bwd_dq_kernel<Elem, L2L_DP, D>, blocks(a, a.heads, 128), a, s);
+      go(sattn::seq_bwd_dkv_kernel<Elem, L2L_DP, D, false>, blocks(a, a.kv_heads, 128), a, s);
+    }
+  };
+  if (a.drop) both(std::true_type{});
+  else both(std::false_type{});
 #endif
 }
