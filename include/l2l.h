@@ -366,7 +366,8 @@ typedef struct {
 } l2l_attention;
 /* o = (softmax(scale q k^T) dropped) v.  q, o: [rows, heads d], k, v: [rows, kv_heads d], each with its own row stride in elements (column
    groups of one QKV matrix do); 16-byte aligned, strides too.  lse: float [heads][rows], the logarithm of each softmax
-   row's denominator (NULL: not wanted; the backward call needs it).  work: l2l_op_attention_work_bytes bytes, 16-byte aligned, or NULL. */
+   row's denominator (NULL: not wanted; the backward call needs it).  work: l2l_op_attention_work_bytes bytes, 16-byte aligned, or NULL,
+   which leaves every row's keys to one workgroup also where there are few rows. */
 int l2l_op_attention(l2l_ctx*, const l2l_attention*, const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv,
                      void* o, long long ldo, float* lse, void* work);
 /* Its gradients: dq [rows, heads d], dk, dv [rows, kv_heads d] (summed over the query heads that share them) from dout, the

@@ -2347,13 +2347,52 @@ static const char* attention_desc_error(const l2l_attention* a) {
   if (!(a->scale > 0.f) || !std::isfinite(a->scale)) return "scale must be positive and finite";
   if (!drop_threshold(a->dropout, 256, &drop)) return "dropout must be 0, or from 1/512 to 511/512 (it is taken to the nearest 1/256)";
   if (((uintptr_t)a->first | (uintptr_t)a->len) & 3 || (uintptr_t)a->step & 7) return "misaligned first, len or step";
-  if ((long long)a->sequences * a->heads * ((a->max_len + 31) / 32) > (1LL << 30)) return "too many (sequence, head, query block)s for one launch";
+  if ((long long)a->sequences * a->heads * ((a->max_len + 127) / 128) > (1LL << 22)) return "too many (sequence, head, query block)s for one launch";
   return nullptr;
+}
+
+// Splits of the attention kernels' long axis: the number with the shortest estimated time.  In tiles of 64 a workgroup's longest walk is
+// `tiles`, and all `wgs` walks together are `total`; a compute unit takes its tiles one after the other, whichever of its workgroups they
+// belong to, so that the launch lasts as long as the longest walk, or as an even share and half a walk more.  Splits shorten the walk, up to
+// four workgroups a compute unit, and cost a launch and their fp32 partial results (`bytes` each).  Measured, whole and chosen splits
+// + their sum (us): one sequence of 2048, 4 query heads on 1 of 64 columns, dropped: forward 40, 18 + 10; dQ 47, 20 + 5; dK and dV
+// 206, 29 + 8.  Two of 1024, 16 heads on 4 of 128: dK and dV 138, 63 + 10; its forward stays whole at 29 (two splits: 31 + 13).  A causal
+// 16384, 32 heads on 8 of 128, stays whole: dK and dV 4520 (two splits: 4445 + 93).
+static int attention_splits(double wgs, int tiles, double total, double us_per_tile, double bytes) {
+  int best_s = 1;
+  double best = 1e300;
+  for (int s = 1; s == 1 || (s <= 16 && tiles / s >= 2 && wgs * s <= 1024); ++s) {
+    const double walk = std::ceil((double)tiles / s);
+    const double us = std::max(walk, total / 256 + walk / 2) * us_per_tile + (s > 1 ? 4.0 + s * bytes / 5.0e6 : 0.0);
+    if (us < best * 0.9) { best = us; best_s = s; }   // (one more has to be worth it)
+  }
+  return best_s;
+}
+
+struct AttentionSplits { int fwd, dq, dkv; size_t fwd_bytes, bwd_bytes; };   // bytes of workspace of either call
+static AttentionSplits attention_plan(const l2l_attention* a) {
+  AttentionSplits p = {1, 1, 1, 0, 0};
+  const double rows = (double)a->rows, q = rows * a->heads, kv = rows * a->kv_heads;
+  const size_t stats = ((size_t)(2 * q) * 4 + 15) / 16 * 16;
+  if (is16(a->dtype) && a->max_len > 0) {
+    // How long the sequences really are only the device knows: max_len and the token rows bound them.
+    const int tiles = (a->max_len + 63) / 64, group = a->heads / a->kv_heads;
+    const double len = std::min((double)a->max_len, rows / a->sequences);
+    const double blocks = std::min(rows / 128 + a->sequences, (double)a->sequences * ((a->max_len + 127) / 128));
+    const double total = blocks * len / 64 * a->heads * (a->causal ? 0.5 : 1.0);
+    const double us = std::max(0.8, a->head_dim / 60.0) + (a->dropout > 0 ? 0.7 : 0.0);   // of a tile (1.1 at 64 columns, 2.1 at 128; 1.8 and 2.4 at 64 and 96 dropped)
+    p.fwd = p.dq = attention_splits(blocks * a->heads, tiles, total, us, q * a->head_dim * 4);
+    p.dkv = attention_splits(blocks * a->kv_heads, tiles * group, total, us, 2 * kv * a->head_dim * 4);
+  }
+  if (p.fwd > 1) p.fwd_bytes = (size_t)(p.fwd * q * (a->head_dim + 1)) * 4;
+  p.bwd_bytes = stats + (size_t)std::max(p.dq > 1 ? p.dq * q * a->head_dim * 4 : 0.0, p.dkv > 1 ? p.dkv * 2 * kv * a->head_dim * 4 : 0.0);
+  return p;
 }
 
 size_t l2l_op_attention_work_bytes(const l2l_attention* a) {
   if (attention_desc_error(a)) return 0;
-  return (size_t)a->heads * (size_t)a->rows * 8;
+  const AttentionSplits p = attention_plan(a);
+  return std::max(p.fwd_bytes, p.bwd_bytes);
 }
 
 // rows of `heads` heads as the kernels read and write them
@@ -2372,6 +2411,7 @@ static SeqAttnArgs attention_args(l2l_ctx* c, const l2l_attention* a, const void
   g.rows = a->rows; g.scale = a->scale;
   (void)drop_threshold(a->dropout, 256, &g.drop);
   g.seed = a->seed; g.site = a->site; g.step = a->step;
+  g.splits_fwd = g.splits_dq = g.splits_dkv = 1;
   g.by_xcd = 2LL * a->max_len * a->head_dim * (long long)esize(a->dtype) >= 2 << 20;   // (half of an XCD's L2)
   g.bad = c->bad_ids;
   return g;
@@ -2403,6 +2443,9 @@ int l2l_op_attention(l2l_ctx* c, const l2l_attention* a, const void* q, long lon
   L2L_TRY(need_device(c, "l2l_op_attention"));
   SeqAttnArgs g = attention_args(c, a, q, ldq, k, ldk, v, ldv);
   g.out = o; g.ldo = ldo; g.lse = lse;
+  g.splits_fwd = work ? attention_plan(a).fwd : 1;
+  g.part = (float*)work;
+  g.part_lse = g.part + (long long)g.splits_fwd * a->rows * a->heads * a->head_dim;
   return timed(c, L2L_PROF_ATTN, 0, 0, [&] { L2L_SEQ_ATTN_PICK(fwd, a->dtype, a->head_dim, g, c->cs); });
 }
 
@@ -2425,8 +2468,11 @@ int l2l_op_attention_bwd(l2l_ctx* c, const l2l_attention* a, const void* q, long
   SeqAttnArgs g = attention_args(c, a, q, ldq, k, ldk, v, ldv);
   g.o = o; g.ldo = ldo; g.lse = (float*)lse; g.dout = dout; g.lddo = lddo;
   g.dq = dq; g.lddq = lddq; g.dk = dk; g.lddk = lddk; g.dv = dv; g.lddv = lddv;
+  const AttentionSplits p = attention_plan(a);
+  g.splits_dq = p.dq; g.splits_dkv = p.dkv;
   g.nlse2 = (float*)work;
   g.delta = g.nlse2 + (long long)a->heads * a->rows;
+  g.part = g.nlse2 + (2 * (long long)a->heads * a->rows + 3) / 4 * 4;
   return timed(c, L2L_PROF_ATTN, 0, 0, [&] { L2L_SEQ_ATTN_PICK(bwd, a->dtype, a->head_dim, g, c->cs); });
 }
 

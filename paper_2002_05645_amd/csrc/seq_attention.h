@@ -136,6 +136,18 @@ struct Tiles {
 };
 __device__ __forceinline__ f32x16 splat16(float x) { return f32x16{x, x, x, x, x, x, x, x, x, x, x, x, x, x, x, x}; }
 
+// the same rows as fp32 partial results, straight from the registers (16 bytes a lane; few of them are written)
+template <int DP>
+__device__ __forceinline__ void store_part(const f32x16 (&acc)[DP / 32], float* row, bool live, int d, int lane, float scale) {
+#pragma unroll
+  for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+    for (int blk = 0; blk < 4; ++blk) {
+      const int col = t * 32 + blk * 8 + 4 * (lane >> 5);
+      if (live && col < d) *(f32x4*)(row + col) = f32x4{acc[t][4 * blk], acc[t][4 * blk + 1], acc[t][4 * blk + 2], acc[t][4 * blk + 3]} * scale;
+    }
+}
+
 // ---- forward -----------------------------------------------------------------------------------------------------------
 // A workgroup owns 128 NQ queries of one (sequence, head), each of its four waves 32 NQ of them, and walks the keys in tiles of 64; the next
 // tile's K and V are on their way into the other half of the LDS while one is computed.
@@ -145,9 +157,10 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
   __shared__ __attribute__((aligned(1024))) char lds[4 * I::IMG];
   const int nblk = (a.max_len + 128 * NQ - 1) / (128 * NQ), group = a.heads / a.kv_heads;
-  const Place at = place(a, group * nblk);
-  const int blk = nblk - 1 - at.block % nblk;   // (a causal sequence's longest blocks first)
-  const int b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads, h = hk * group + at.block / nblk, bh = b * a.heads + h;
+  const Place at = place(a, group * nblk * a.splits_fwd);
+  const int split = at.block % a.splits_fwd, of_head = at.block / a.splits_fwd;
+  const int blk = nblk - 1 - of_head % nblk;   // (a causal sequence's longest blocks first)
+  const int b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads, h = hk * group + of_head / nblk, bh = b * a.heads + h;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_q = blk * 128 * NQ;
   if (base_q >= n) return;
@@ -155,27 +168,29 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
   const int q0 = base_q + wave * 32 * NQ;
   const bool active = q0 < n;   // (per wave)
   const Tiles<E, DP> kt(a.k, sq.first, a.ldk, hk, n, a.d, wave, lane), vt(a.v, sq.first, a.ldv, hk, n, a.d, wave, lane);
-  const int last = a.causal ? min(n, base_q + 128 * NQ) : n, tiles = (last + CHA - 1) / CHA;
+  const int last = a.causal ? min(n, base_q + 128 * NQ) : n, all_tiles = (last + CHA - 1) / CHA;
+  const int from = all_tiles * split / a.splits_fwd, tiles = all_tiles * (split + 1) / a.splits_fwd;   // this split's
   const uint32_t lds0 = lds_place((const __attribute__((address_space(3))) char*)lds);
   const auto fetch = [&](int t) {
     const uint32_t to = lds0 + (t & 1) * 2 * I::IMG;
     kt.fetch(t * CHA, to, wave);
     vt.fetch(t * CHA, to + I::IMG, wave);
   };
-  fetch(0);
+  if (from < tiles) fetch(from);
   bf16x8 qf[NQ][DP / 16];
   f32x16 o[NQ][DP / 32];
   float m[NQ], sum[NQ];
+  // No row's maximum yet: far below any score, and finite, as a split's first tile may have no key that the row sees.
+  const float c = a.scale * LOG2E, lowest = fmaxf(-1e30f / c, -1e38f);
 #pragma unroll
   for (int u = 0; u < NQ; ++u) {
     const int q = q0 + u * 32 + (lane & 31);
     I::template row_frags<E>((const E*)a.q + (sq.first + q) * a.ldq + (long long)h * a.d, q < n, a.d, lane, qf[u]);
-    m[u] = -INFINITY;
+    m[u] = lowest;
     sum[u] = 0.f;
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) o[u][t] = zero16();
   }
-  const float c = a.scale * LOG2E;
   DropKey key;
   if (DROP) key = drop_key(a.seed, a.site, a.step);
   const auto arrive = [&](int t) {
@@ -264,8 +279,8 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
   // The wave's tiles: those that all of its queries see whole, those with a mask, and those of its neighbours', where it only helps to
   // load.  In loops of their own: with the mask and the way round the work as branches inside one, the accumulators are copied back and forth.
   const int mine = !active ? 0 : a.causal ? min(tiles, (q0 + 32 * NQ + CHA - 1) / CHA) : tiles;
-  const int whole = min(mine, (a.causal ? min(n, q0 + 1) : n) / CHA);
-  int t = 0;
+  const int whole = min(mine, (a.causal ? min(n, q0 + 1) : n) / CHA);   // (counted from the first key, whatever the split)
+  int t = from;
   for (; t < whole; ++t) { arrive(t); compute(t, std::false_type{}); }
   for (; t < mine; ++t) { arrive(t); compute(t, std::true_type{}); }
   for (; t < tiles; ++t) arrive(t);
@@ -277,6 +292,13 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
     const int qr = q0 + u * 32, q = qr + (lane & 31);
     if (qr >= n) break;
     const float l = half_sum(sum[u]);
+    if (a.splits_fwd > 1) {   // (a split without a key that the row sees: l = 0)
+      const bool live = q < n, none = l == 0.f;
+      const long long row = (long long)split * a.rows + sq.first + q;
+      store_part<DP>(o[u], a.part + row * ((long long)a.heads * a.d) + (long long)h * a.d, live, a.d, lane, none ? 0.f : kept / l);
+      if (lane < 32 && live) a.part_lse[((long long)split * a.heads + h) * a.rows + sq.first + q] = none ? -INFINITY : (m[u] * c + __builtin_amdgcn_logf(l)) * LN2;
+      continue;
+    }
     store_rows<E, DP>(o[u], lds + wave * I::IMG, (E*)a.out + (sq.first + qr) * a.ldo + (long long)h * a.d, a.ldo, n - qr, a.d, lane, kept / l);
     if (a.lse && lane < 32 && q < n) a.lse[(long long)h * a.rows + sq.first + q] = (m[u] * c + __builtin_amdgcn_logf(l)) * LN2;
   }
@@ -289,9 +311,10 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
   __shared__ __attribute__((aligned(1024))) char lds[4 * I::IMG];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, group * nblk);
-  const int blk = nblk - 1 - at.block % nblk;
-  const int b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads, h = hk * group + at.block / nblk, bh = b * a.heads + h;
+  const Place at = place(a, group * nblk * a.splits_dq);
+  const int split = at.block % a.splits_dq, of_head = at.block / a.splits_dq;
+  const int blk = nblk - 1 - of_head % nblk;
+  const int b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads, h = hk * group + of_head / nblk, bh = b * a.heads + h;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_q = blk * 128;
   if (base_q >= n) return;
@@ -299,14 +322,15 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
   const int q0 = base_q + wave * 32, q = q0 + (lane & 31);
   const bool active = q0 < n;
   const Tiles<E, DP> kt(a.k, sq.first, a.ldk, hk, n, a.d, wave, lane), vt(a.v, sq.first, a.ldv, hk, n, a.d, wave, lane);
-  const int last = a.causal ? min(n, base_q + 128) : n, tiles = (last + CHA - 1) / CHA;
+  const int last = a.causal ? min(n, base_q + 128) : n, all_tiles = (last + CHA - 1) / CHA;
+  const int from = all_tiles * split / a.splits_dq, tiles = all_tiles * (split + 1) / a.splits_dq;
   const uint32_t lds0 = lds_place((const __attribute__((address_space(3))) char*)lds);
   const auto fetch = [&](int t) {
     const uint32_t to = lds0 + (t & 1) * 2 * I::IMG;
     kt.fetch(t * CHA, to, wave);
     vt.fetch(t * CHA, to + I::IMG, wave);
   };
-  fetch(0);
+  if (from < tiles) fetch(from);
   bf16x8 qf[DP / 16], gf[DP / 16];
   const E* grow = (const E*)a.dout + (sq.first + q) * a.lddo + (long long)h * a.d;
   const E* orow = (const E*)a.o + (sq.first + q) * a.ldo + (long long)h * a.d;
@@ -327,7 +351,8 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
     nl = -a.lse[(long long)h * a.rows + sq.first + q] / a.scale;
   }
   D = half_sum(D);
-  if (q < n && lane < 32) {
+  const bool stats = q < n && lane < 32 && from == 0 && tiles > 0;   // (one of the splits writes them)
+  if (stats) {
     a.nlse2[(long long)h * a.rows + sq.first + q] = nl;
     a.delta[(long long)h * a.rows + sq.first + q] = -D;
   }
@@ -371,6 +396,21 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) g[r] *= s[r];
       }
+      // D comes from O as it was stored, off by its rounding: noise in every dS of the row, which is one over the square root of the number of keys of
+      // what dS's own rounding does, but all of it where rows see few.  A row of dS has the sum zero (P has the sum 1): where these 32
+      // keys are all that the rows see, its sum is D's error, and is taken out.  (Two to four keys: the gradients' error falls from
+      // 1.6 times that of their rounding alone, against 64 bits, to the 1.4 of long rows.)
+      if constexpr (decltype(edge)::value) {
+        if (kb == 0 && q0 == 0 && (a.causal || n <= 32)) {
+          float off = 0.f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) off += g[r];
+          off = half_sum(off);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) g[r] = fmaf(-s[r], off, g[r]);
+          if (stats) a.delta[(long long)h * a.rows + sq.first + q] = -(D + off);
+        }
+      }
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
         const bf16x8 df = pack8<E>(g, 8 * s2);
@@ -382,12 +422,17 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
   };
   const int mine = !active ? 0 : a.causal ? min(tiles, (q0 + 32 + CHA - 1) / CHA) : tiles;   // (as in the forward kernel)
   const int whole = min(mine, (a.causal ? min(n, q0 + 1) : n) / CHA);
-  int t = 0;
+  int t = from;
   for (; t < whole; ++t) { arrive(t); compute(t, std::false_type{}); }
   for (; t < mine; ++t) { arrive(t); compute(t, std::true_type{}); }
   for (; t < tiles; ++t) arrive(t);
   __syncthreads();
   if (!active) return;
+  if (a.splits_dq > 1) {
+    const long long row = (long long)split * a.rows + sq.first + q;
+    store_part<DP>(dq, a.part + row * ((long long)a.heads * a.d) + (long long)h * a.d, q < n, a.d, lane, a.scale);
+    return;
+  }
   store_rows<E, DP>(dq, lds + wave * I::IMG, (E*)a.dq + (sq.first + q0) * a.lddq + (long long)h * a.d, a.lddq, n - q0, a.d, lane, a.scale);
 }
 
@@ -405,8 +450,8 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   constexpr int KIMG = 2 * STAGE, SIMG = KIMG + 2 * I::IMG, STAT = SIMG + 2 * IS::IMG;   // (WHOLE) K, dS, two heads' -lse and D of 128 rows
   __shared__ __attribute__((aligned(1024))) char lds[WHOLE ? STAT + 2 * 1024 : 2 * STAGE];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, nblk);
-  const int blk = at.block, b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads;
+  const Place at = place(a, nblk * a.splits_dkv);
+  const int split = at.block % a.splits_dkv, blk = at.block / a.splits_dkv, b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_k = blk * 128;
   if (base_k >= n) return;
@@ -414,10 +459,12 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   const int key0 = base_k + wave * 32, kk = key0 + (lane & 31);
   const bool active = key0 < n;
   // query tiles of one head: with a causal mask from the one that holds this block's first key on
-  const int t0 = a.causal ? base_k / CHA : 0, per_head = (n + CHA - 1) / CHA - t0, tiles = per_head * group;
-  Tiles<E, DP> qt(a.q, sq.first, a.ldq, hk * group, n, a.d, wave, lane), gt(a.dout, sq.first, a.lddo, hk * group, n, a.d, wave, lane);
-  const float* stats = (wave ? a.delta : a.nlse2) + (long long)hk * group * a.rows + sq.first;
-  int next_t = t0;   // the next tile to be fetched, of the head that the three point at
+  const int t0 = a.causal ? base_k / CHA : 0, per_head = (n + CHA - 1) / CHA - t0, all_tiles = per_head * group;
+  const int from = all_tiles * split / a.splits_dkv, tiles = all_tiles * (split + 1) / a.splits_dkv - from;   // this split's, of all heads' in turn
+  const int h0 = hk * group + from / per_head;
+  Tiles<E, DP> qt(a.q, sq.first, a.ldq, h0, n, a.d, wave, lane), gt(a.dout, sq.first, a.lddo, h0, n, a.d, wave, lane);
+  const float* stats = (wave ? a.delta : a.nlse2) + (long long)h0 * a.rows + sq.first;
+  int next_t = t0 + from % per_head;   // the next tile to be fetched, of the head that the three point at
   const uint32_t lds0 = lds_place((const __attribute__((address_space(3))) char*)lds);
   const auto fetch = [&](int i) {
     const uint32_t to = lds0 + (i & 1) * STAGE;
@@ -432,7 +479,7 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
       stats += a.rows;
     }
   };
-  fetch(0);
+  if (tiles > 0) fetch(0);
   if constexpr (WHOLE) {
     const Tiles<E, DP> kt(a.k, sq.first, a.ldk, hk, n, a.d, wave, lane);
     kt.fetch(0, lds0 + KIMG, wave);
@@ -460,6 +507,7 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
     float* st = (float*)(lds + STAT + (h & 1) * 1024);
     st[half * 128 + row] = half ? -D : nl;
   };
+  const bool few = key0 == 0 && (a.causal || n <= 32);   // the wave's keys are all that the first 32 rows see
   bf16x8 kf[DP / 16], vf[DP / 16];
   I::template row_frags<E>((const E*)a.k + (sq.first + kk) * a.ldk + (long long)hk * a.d, kk < n, a.d, lane, kf);
   I::template row_frags<E>((const E*)a.v + (sq.first + kk) * a.ldv + (long long)hk * a.d, kk < n, a.d, lane, vf);
@@ -480,7 +528,7 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
     const char* Gs = Qs + I::IMG;
     const float* Ls = WHOLE ? (const float*)(lds + STAT + (h & 1) * 1024) + row0 : (const float*)(Gs + I::IMG);
     const float* Ds = Ls + (WHOLE ? 128 : 64);
-    const int lim = kk - row0 - 4 * (lane >> 5);   // causal: rows below it do not see this lane's key
+    const int lim = a.causal ? kk - row0 - 4 * (lane >> 5) : 0;   // causal: rows below it do not see this lane's key
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
       f32x16 s, g;   // (from -lse / scale and -D, as in the dQ kernel)
@@ -503,8 +551,9 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
         for (int r = 0; r < 16; ++r)
           if (qb * 32 + 8 * (r >> 2) + (r & 3) < lim) s[r] = 0.f;
       }
+      u32x4 bytes;
       if (DROP) {
-        const u32x4 bytes = drop_bytes<false>(row0 + qb * 32, key0, (uint32_t)(b * a.heads + h), key, lane);
+        bytes = drop_bytes<false>(row0 + qb * 32, key0, (uint32_t)(b * a.heads + h), key, lane);
 #pragma unroll
         for (int blk4 = 0; blk4 < 4; ++blk4) {
           const f32x4 D4 = *(const f32x4*)(Ds + qb * 32 + 8 * blk4 + 4 * (lane >> 5));
@@ -513,12 +562,30 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
             const int r = 4 * blk4 + j;
             const bool keep = drop_keeps(bytes, r, a.drop);
             g[r] = s[r] * (keep ? fmaf(g[r], kept, D4[j]) : D4[j]);
-            s[r] = drop_select(keep, s[r]);
+            if (!(WHOLE && decltype(edge)::value)) s[r] = drop_select(keep, s[r]);
           }
         }
       } else {
 #pragma unroll
         for (int r = 0; r < 16; ++r) g[r] *= s[r];
+      }
+      if constexpr (WHOLE && decltype(edge)::value) {
+        if (qb == 0 && few && row0 == 0) {   // D's error, as in the dQ kernel: the row's keys are this wave's lanes
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            float off = kk < n ? g[r] : 0.f;
+            off += dpp_move<0xB1>(off);
+            off += dpp_move<0x4E>(off);
+            off += dpp_move<0x141>(off);
+            off += dpp_move<0x140>(off);
+            off += __shfl_xor(off, 16);
+            g[r] = fmaf(-s[r], off, g[r]);
+          }
+        }
+        if (DROP) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = drop_select(drop_keeps(bytes, r, a.drop), s[r]);
+        }
       }
       if (WHOLE && key0 + 32 > n) {   // a key past the sequence has a row of K that is zero, and a dS that may be anything
 #pragma unroll
@@ -575,22 +642,79 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   };
   // per head: tiles before the wave's first key, where it only helps to load, those with a mask, those whole
   const int idle = !active ? per_head : a.causal ? min(per_head, key0 / CHA - t0) : 0;
-  const int masked = a.causal ? min(per_head, (key0 + 31 + CHA - 1) / CHA - t0) : 0;
-  for (int h = hk * group; h < (hk + 1) * group; ++h) {
-    int t = 0;
+  const int masked = a.causal ? min(per_head, (key0 + 31 + CHA - 1) / CHA - t0) : WHOLE && few ? 1 : 0;   // (the first tile: D's error)
+  for (int h = h0; i < tiles; ++h) {
+    int t = h == h0 ? from % per_head : 0;
+    const int end = min(per_head, t + tiles - i);
     if (WHOLE) head_stats(h);
     const auto grads = [&] {
       if constexpr (WHOLE) query_grads(h, (t0 + t) * CHA);
     };
-    for (; t < idle; ++t, ++i) { arrive(); grads(); }
-    for (; t < masked; ++t, ++i) { arrive(); compute(h, (t0 + t) * CHA, std::true_type{}); grads(); }
-    for (; t < per_head; ++t, ++i) { arrive(); compute(h, (t0 + t) * CHA, std::false_type{}); grads(); }
+    for (; t < min(idle, end); ++t, ++i) { arrive(); grads(); }
+    for (; t < min(masked, end); ++t, ++i) { arrive(); compute(h, (t0 + t) * CHA, std::true_type{}); grads(); }
+    for (; t < end; ++t, ++i) { arrive(); compute(h, (t0 + t) * CHA, std::false_type{}); grads(); }
   }
   __syncthreads();
   if (!active) return;
+  if (a.splits_dkv > 1) {
+    const long long width = (long long)a.kv_heads * a.d, row = 2LL * split * a.rows + sq.first + kk;
+    store_part<DP>(dv, a.part + row * width + (long long)hk * a.d, kk < n, a.d, lane, kept);
+    store_part<DP>(dk, a.part + (row + a.rows) * width + (long long)hk * a.d, kk < n, a.d, lane, a.scale);
+    return;
+  }
   char* stage = lds + wave * (STAGE / 2);
   store_rows<E, DP>(dv, stage, (E*)a.dv + (sq.first + key0) * a.lddv + (long long)hk * a.d, a.lddv, n - key0, a.d, lane, kept);
   store_rows<E, DP>(dk, stage, (E*)a.dk + (sq.first + key0) * a.lddk + (long long)hk * a.d, a.lddk, n - key0, a.d, lane, a.scale);
+}
+
+// ---- partial results of the splits together -------------------------------------------------------------------------------
+// out = sum over the splits of part, or with WEIGHTED (forward) of e^(lse_s - lse) part_s, lse = log sum e^lse_s.  A workgroup takes 64
+// rows of one (sequence, head), eight columns a thread; splits in their order.  Bound by memory, the splits' share of it.
+struct JoinArgs {
+  const float* part[2];     // of dV and dK; otherwise one
+  long long split_stride;   // elements from a split to the next
+  const float* part_lse;    // WEIGHTED
+  float* lse;               // WEIGHTED: or null
+  void* out[2];
+  long long ldo[2];
+  int splits, heads;        // heads of `out`
+};
+template <typename E, bool WEIGHTED>
+__global__ __launch_bounds__(256) void seq_join_kernel(const SeqAttnArgs a, const JoinArgs j) {
+  const int nblk = (a.max_len + 63) / 64, blk = blockIdx.x % nblk, bh = blockIdx.x / nblk, b = bh / j.heads, h = bh % j.heads;
+  const float* part = j.part[blockIdx.y];
+  E* out = (E*)j.out[blockIdx.y];
+  const long long ldo = j.ldo[blockIdx.y];
+  const Seq sq = sequence(a, b);
+  const int chunks = a.d / 8;
+  for (int u = threadIdx.x; u < 64 * chunks; u += 256) {
+    const int i = blk * 64 + u / chunks, col = u % chunks * 8;
+    if (i >= sq.n) return;
+    const long long row = sq.first + i, at = row * ((long long)j.heads * a.d) + (long long)h * a.d + col;
+    float top = -INFINITY, total = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (WEIGHTED) {
+      for (int s = 0; s < j.splits; ++s) top = fmaxf(top, j.part_lse[((long long)s * j.heads + h) * a.rows + row]);
+    }
+    for (int s = 0; s < j.splits; ++s) {
+      float w = 1.f;
+      if (WEIGHTED) {
+        const float l = j.part_lse[((long long)s * j.heads + h) * a.rows + row];
+        if (l == -INFINITY) continue;   // (nothing was stored)
+        w = __builtin_amdgcn_exp2f((l - top) * LOG2E);
+        total += w;
+      }
+      float v[8];
+      load8(part + s * j.split_stride + at, v);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) acc[x] = fmaf(v[x], w, acc[x]);
+    }
+    if (WEIGHTED) {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) acc[x] /= total;
+      if (j.lse && col == 0) j.lse[(long long)h * a.rows + row] = top + __builtin_amdgcn_logf(total) * LN2;
+    }
+    store8(out + row * ldo + (long long)h * a.d + col, acc);
+  }
 }
 
 }  // namespace sattn

@@ -26,6 +26,14 @@ dim3 blocks(const SeqAttnArgs& a, int heads, int rows_per) {
   return dim3((unsigned)((long long)a.sequences * heads * ((a.max_len + rows_per - 1) / rows_per)));
 }
 
+#if L2L_ELEM != 0
+template <bool WEIGHTED>
+void join(const SeqAttnArgs& a, const sattn::JoinArgs& j, hipStream_t s) {
+  const dim3 grid((unsigned)((long long)a.sequences * j.heads * ((a.max_len + 63) / 64)), j.out[1] ? 2 : 1);
+  hipLaunchKernelGGL((sattn::seq_join_kernel<Elem, WEIGHTED>), grid, dim3(256), 0, s, a, j);
+}
+#endif
+
 template <typename K>
 void go(K kern, dim3 grid, const SeqAttnArgs& a, hipStream_t s) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a); }
 
@@ -36,8 +44,10 @@ void L2L_NAME(l2l_seq_attn_fwd_)(const SeqAttnArgs& a, hipStream_t s) {
   if (a.drop) go(sattn::seq_fwd_f32_kernel<L2L_DP, true>, blocks(a, a.heads, 128), a, s);
   else go(sattn::seq_fwd_f32_kernel<L2L_DP, false>, blocks(a, a.heads, 128), a, s);
 #else
-  if (a.drop) go(sattn::seq_fwd_kernel<Elem, L2L_DP, 1, true>, blocks(a, a.heads, 128), a, s);
-  else go(sattn::seq_fwd_kernel<Elem, L2L_DP, 1, false>, blocks(a, a.heads, 128), a, s);
+  if (a.drop) go(sattn::seq_fwd_kernel<Elem, L2L_DP, 1, true>, blocks(a, a.heads * a.splits_fwd, 128), a, s);
+  else go(sattn::seq_fwd_kernel<Elem, L2L_DP, 1, false>, blocks(a, a.heads * a.splits_fwd, 128), a, s);
+  if (a.splits_fwd > 1)
+    join<true>(a, {{a.part}, a.rows * a.heads * a.d, a.part_lse, a.lse, {a.out}, {a.ldo}, a.splits_fwd, a.heads}, s);
 #endif
 }
 
@@ -54,14 +64,19 @@ void L2L_NAME(l2l_seq_attn_bwd_)(const SeqAttnArgs& a, hipStream_t s) {
   const auto both = [&](auto drop) {
     constexpr bool D = decltype(drop)::value;
     if constexpr (L2L_DP <= 64) {   // (wider heads leave no registers for it)
-      if (a.max_len <= 128) {       // a workgroup has all of a head's keys: one kernel does both
+      if (a.max_len <= 128 && a.splits_dkv == 1) {       // a workgroup has all of a head's keys: one kernel does both
         go(sattn::seq_bwd_dkv_kernel<Elem, L2L_DP, D, true>, blocks(a, a.kv_heads, 128), a, s);
         return;
       }
     }
     {
-      go(sattn::seq_bwd_dq_kernel<Elem, L2L_DP, D>, blocks(a, a.heads, 128), a, s);
-      go(sattn::seq_bwd_dkv_kernel<Elem, L2L_DP, D, false>, blocks(a, a.kv_heads, 128), a, s);
+      go(sattn::seq_bwd_dq_kernel<Elem, L2L_DP, D>, blocks(a, a.heads * a.splits_dq, 128), a, s);
+      if (a.splits_dq > 1) join<false>(a, {{a.part}, a.rows * a.heads * a.d, nullptr, nullptr, {a.dq}, {a.lddq}, a.splits_dq, a.heads}, s);
+      go(sattn::seq_bwd_dkv_kernel<Elem, L2L_DP, D, false>, blocks(a, a.kv_heads * a.splits_dkv, 128), a, s);
+      if (a.splits_dkv > 1) {
+        const long long one = a.rows * a.kv_heads * a.d;
+        join<false>(a, {{a.part, a.part + one}, 2 * one, nullptr, nullptr, {a.dv, a.dk}, {a.lddv, a.lddk}, a.splits_dkv, a.kv_heads}, s);
+      }
     }
   };
   if (a.drop) both(std::true_type{});

@@ -211,6 +211,95 @@ def test_attention_rows_far_behind_32_bit_offsets(ctx):
     small.check()
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype,heads,kv,d", [("bf16", 4, 1, 64), ("fp16", 3, 3, 96), ("bf16", 2, 2, 32), ("fp16", 4, 2, 128), ("bf16", 3, 1, 40), ("fp16", 1, 1, 8)])
+def test_attention_few_workgroups_share_the_long_axis(ctx, dtype, heads, kv, d, causal):
+    # so few (sequence, head, block)s that the workgroups take parts of the keys, or of the queries, and a second kernel adds them up; splits that end
+    # in the middle of a causal row, and short sequences whose splits are empty
+    for p in (0.0, 0.3):
+        x = Problem(dtype, heads, kv, d, [1100, 0, 1, 65, 130, 897], causal, p, gaps=[1, 0, 3, 0, 2, 1], pad_cols=8, seed=d, amp=1.5)
+        assert x.work.numel() >= heads * x.rows * 8 + 2 * heads * x.rows * d * 4
+        x.forward(ctx)
+        x.backward(ctx)
+        ctx.sync()
+        x.check()
+
+
+def test_attention_forward_without_workspace_is_not_split(ctx):
+    x = Problem("bf16", 2, 2, 64, [1500], False, 0.2, seed=2)
+    x.work, keep = None, x.work
+    x.forward(ctx)
+    x.work = keep
+    x.backward(ctx)
+    ctx.sync()
+    x.check()
+
+
+@pytest.mark.parametrize("dtype,heads,kv,d", [("bf16", 4, 2, 64), ("fp16", 6, 2, 32), ("bf16", 3, 1, 40)])
+def test_attention_backward_in_one_kernel(ctx, dtype, heads, kv, d):
+    # every sequence's keys fit one workgroup; lengths around the tile and wave edges, shared key heads, and a batch that leaves rows out
+    for causal in (False, True):
+        for p in (0.0, 0.3):
+            x = Problem(dtype, heads, kv, d, [128, 127, 97, 96, 65, 64, 63, 33, 32, 31, 2, 1, 0, 100], causal, p, gaps=[0, 1] * 7, pad_cols=8, seed=heads)
+            x.forward(ctx)
+            x.backward(ctx)
+            ctx.sync()
+            x.check()
+
+
+@pytest.mark.parametrize("dtype,d,longest", [("bf16", 64, 33), ("fp16", 32, 128), ("bf16", 96, 40), ("fp16", 128, 32), ("bf16", 64, 600)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_one_key_has_no_score_gradient(ctx, dtype, d, longest, causal):
+    # a row that sees one key has the probability 1 whatever its score: dS = 0, although D = dO . O comes from a rounded O
+    for p in (0.0, 0.4):
+        x = Problem(dtype, 2, 1, d, [1, longest, 1, 20, 1], causal, p, seed=longest, amp=2.0)
+        x.forward(ctx)
+        x.backward(ctx)
+        ctx.sync()
+        x.check()
+        for b, n in enumerate(x.lengths):
+            if n > 1 and not causal:
+                continue
+            r = x.first[b]
+            for h in range(2):
+                c = slice(h * d, h * d + d)
+                q, do, dq = (to_host(m[r, c]) for m in (x.q, x.do, x.dq))
+                k, v = to_host(x.k[r, :d]), to_host(x.v[r, :d])
+                # dP and D: sums of d terms and O's rounding; P = 1 within the fp32 work of one exponential; what is left of dS is their product
+                f = (d + 64 + 8 * d ** -0.5 * (np.abs(q) @ np.abs(k))) * E24
+                dP = np.abs(do) @ np.abs(v) / (1 - p)
+                tol = d ** -0.5 * np.abs(k) * ((U[dtype] + f) * dP * f + 4 * E24 * (U[dtype] + f) * dP) * 2 + LOW[dtype]
+                assert (np.abs(dq) <= tol).all(), (b, h, (np.abs(dq) / tol).max())
+
+
+@pytest.mark.parametrize("heads,kv", [(9, 9), (16, 8), (18, 9)])
+def test_attention_workgroups_by_xcd(ctx, heads, kv):
+    # keys of one head that fill half an L2, and key heads that do not come in eights: every (head, block) is run once
+    n, d = 8200, 128
+    g = torch.Generator().manual_seed(heads)
+    q, k, v = (torch.randn(n, h * d, generator=g).bfloat16().cuda() for h in (heads, kv, kv))
+    o = torch.full((n, heads * d), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((heads, n), 7.0, device="cuda")
+    plan = P.make_attention(dtype="bf16", heads=heads, kv_heads=kv, head_dim=d, sequences=1, max_len=n, rows=n)
+    ctx.op_attention(plan, q, heads * d, k, kv * d, v, kv * d, o, heads * d, lse)
+    ctx.sync()
+    rows = [0, 31, 127, 128, 4095, 8063, 8064, 8191, 8192, 8199]
+    for h in range(heads):
+        c, ck = slice(h * d, h * d + d), slice(h // (heads // kv) * d, h // (heads // kv) * d + d)
+        Q, K, V = to_host(q[rows][:, c]), to_host(k[:, ck]), to_host(v[:, ck])
+        S = (Q @ K.T) * d ** -0.5
+        top = S.max(-1, keepdims=True)
+        prob = np.exp(S - top)
+        ref = (prob / prob.sum(-1, keepdims=True)) @ V
+        ref_lse = top[:, 0] + np.log(prob.sum(-1))
+        absv = (prob / prob.sum(-1, keepdims=True)) @ np.abs(V)
+        # P rounded to the format, sums of n and d terms in fp32, the result rounded
+        f = ((n + d + 32) + 8 * np.abs(S).max()) * E24
+        assert (np.abs(to_host(o[rows][:, c]) - ref) <= (U["bf16"] + f) * absv * (1 + U["bf16"]) + U["bf16"] * np.abs(ref)).all(), h
+        assert (np.abs(to_host(lse[h][rows]) - ref_lse) <= (d + n + 32 + 2 * np.abs(S).max()) * E24 + E24 * np.abs(ref_lse)).all(), h
+    assert not (o == 7.0).all(-1).any()
+
+
 def test_attention_same_call_gives_the_same_bits(ctx):
     x = Problem("bf16", 8, 2, 64, [300, 257, 64], True, 0.1, seed=6)
     x.forward(ctx)
