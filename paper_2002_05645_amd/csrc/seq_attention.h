@@ -152,7 +152,7 @@ __device__ __forceinline__ void store_part(const f32x16 (&acc)[DP / 32], float* 
 // A workgroup owns 128 NQ queries of one (sequence, head), each of its four waves 32 NQ of them, and walks the keys in tiles of 64; the next
 // tile's K and V are on their way into the other half of the LDS while one is computed.
 template <typename E, int DP, int NQ, bool DROP>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 64 && NQ == 1 ? (DROP ? 3 : 4) : 2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 64 ? 4 : 2)))
 void seq_fwd_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
   __shared__ __attribute__((aligned(1024))) char lds[4 * I::IMG];
@@ -202,79 +202,49 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
     const int k0 = t * CHA;
     const char* Ks = lds + (t & 1) * 2 * I::IMG;
     const char* Vs = Ks + I::IMG;
-    f32x16 s[NQ][2];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
+      f32x16 s = zero16();
 #pragma unroll
-      for (int u = 0; u < NQ; ++u) s[u][kb] = zero16();
+      for (int st = 0; st < DP / 16; ++st) s = mfma_32x32x16<E>(I::rows_frag(Ks, kb * 32 + (lane & 31), st, lane), qf[0][st], s);
+      if constexpr (decltype(edge)::value) {   // keys that a query does not see
+        const int q = q0 + (lane & 31), lim = (a.causal ? min(n, q + 1) : n) - k0 - 4 * (lane >> 5);
 #pragma unroll
-      for (int st = 0; st < DP / 16; ++st) {
-        const bf16x8 kf = I::rows_frag(Ks, kb * 32 + (lane & 31), st, lane);
-#pragma unroll
-        for (int u = 0; u < NQ; ++u) s[u][kb] = mfma_32x32x16<E>(kf, qf[u][st], s[u][kb]);
+        for (int r = 0; r < 16; ++r)
+          if (kb * 32 + 8 * (r >> 2) + (r & 3) >= lim) s[r] = -INFINITY;
       }
-    }
-    if constexpr (decltype(edge)::value) {   // keys that a query does not see
+      float cm = s[0];
 #pragma unroll
-      for (int u = 0; u < NQ; ++u) {
-        const int q = q0 + u * 32 + (lane & 31), lim = (a.causal ? min(n, q + 1) : n) - k0 - 4 * (lane >> 5);
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (kb * 32 + 8 * (r >> 2) + (r & 3) >= lim) s[u][kb][r] = -INFINITY;
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < NQ; ++u) {
-      float cm = s[u][0][0];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) cm = fmaxf(cm, s[u][kb][r]);
-      cm = fmaxf(half_max(cm), m[u]);
-      // The row's maximum only keeps the exponents in range: it moves, and the accumulators are rescaled, when some row of
-      // the wave has exceeded its own by 2^8, which the first tile does and few after it (fp32 sums hold 2^8 as well as 1,
-      // and so does P in either 16-bit format).
-      if (__any((cm - m[u]) * c > 8.0f)) {
-        const float rescale = __builtin_amdgcn_exp2f((m[u] - cm) * c);   // 0 on the first tile
-        m[u] = cm;
-        sum[u] *= rescale;
+      for (int r = 1; r < 16; ++r) cm = fmaxf(cm, s[r]);
+      cm = fmaxf(half_max(cm), m[0]);
+      if (__any((cm - m[0]) * c > 8.0f)) {
+        const float rescale = __builtin_amdgcn_exp2f((m[0] - cm) * c);   // 0 on the first tile
+        m[0] = cm;
+        sum[0] *= rescale;
 #pragma unroll
         for (int t2 = 0; t2 < DP / 32; ++t2)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) o[u][t2][r] *= rescale;
+          for (int r = 0; r < 16; ++r) o[0][t2][r] *= rescale;
       }
-      const float mc = m[u] * c;
+      const float mc = m[0] * c;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[u][kb][r] = __builtin_amdgcn_exp2f(fmaf(s[u][kb][r], c, -mc));
-          sum[u] += s[u][kb][r];
-        }
-        if (DROP) {
-          const u32x4 bytes = drop_bytes<true>(q0 + u * 32, k0 + kb * 32, (uint32_t)bh, key, lane);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[u][kb][r] = drop_select(drop_keeps(bytes, r, a.drop), s[u][kb][r]);
-        }
+      for (int r = 0; r < 16; ++r) {
+        s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -mc));
+        sum[0] += s[r];
       }
-    }
-    // (P is rounded to the format here, as the matrix cores take it: half a step relative, of either sign, per probability)
+      if (DROP) {
+        const u32x4 bytes = drop_bytes<true>(q0, k0 + kb * 32, (uint32_t)bh, key, lane);
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+        for (int r = 0; r < 16; ++r) s[r] = drop_select(drop_keeps(bytes, r, a.drop), s[r]);
+      }
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2) {
-        bf16x8 pf[NQ];
+        const bf16x8 pf = pack8<E>(s, 8 * s2);
 #pragma unroll
-        for (int u = 0; u < NQ; ++u) pf[u] = pack8<E>(s[u][kb], 8 * s2);
-#pragma unroll
-        for (int t2 = 0; t2 < DP / 32; ++t2) {
-          const bf16x8 vf = I::rows_T(Vs, kb, s2, t2, lane);
-#pragma unroll
-          for (int u = 0; u < NQ; ++u) o[u][t2] = mfma_32x32x16<E>(vf, pf[u], o[u][t2]);
-        }
+        for (int t2 = 0; t2 < DP / 32; ++t2) o[0][t2] = mfma_32x32x16<E>(I::rows_T(Vs, kb, s2, t2, lane), pf, o[0][t2]);
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
   // The wave's tiles: those that all of its queries see whole, those with a mask, and those of its neighbours', where it only helps to
   // load.  In loops of their own: with the mask and the way round the work as branches inside one, the accumulators are copied back and forth.
