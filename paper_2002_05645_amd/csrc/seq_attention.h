@@ -38,17 +38,22 @@ __device__ __forceinline__ Halves halves(float v) {
 __device__ __forceinline__ float half_max(float v) { const Halves h = halves(v); return fmaxf(h.lo, h.hi); }
 __device__ __forceinline__ float half_sum(float v) { const Halves h = halves(v); return h.lo + h.hi; }
 
-// Workgroup order.  Consecutive workgroups go to the 8 XCDs in turn, which spreads long and short sequences over the chip: the
-// order is (sequence, key head, query head of it, block) as it stands.  Only where a head's keys and values are the larger part of
-// an L2 does each XCD get whole (sequence, key head) units instead, as far as they come in eights, so that the blocks that read
-// the same ones meet there (one causal sequence of 16384 tokens, 8 key heads of 128: forward 2650 us in turn, 2200 so, dQ 4540 and 3400,
-// dK / dV 6500 and 4600; but 7 sequences of 1 to 1999 tokens, 4 key heads of 96: forward 79 and 151, dQ 87 and 165, dK / dV 240 and 298).
+// Workgroup order.  Consecutive workgroups go to the 8 XCDs in turn, which spreads long and short sequences over the chip: with xcd_run
+// 0 the order is (sequence, key head, query head of it, block) as it stands.  Otherwise an XCD takes xcd_run whole (sequence, key
+// head) units one after the other, as far as runs of them come in eights:
+// - 1 where a head's keys and values are the larger part of an L2: the blocks that read the same ones meet there.  One causal sequence of
+//   16384 tokens, 8 key heads of 128: forward 2650 us in turn, 2200 so, dQ 4540 and 3400, dK and dV 6500 and 4600.
+// - 8 or, with several blocks to a unit, 2 where there are many units (256): heads that lie side by side in memory are read by one XCD
+//   at a time.  256 sequences of 128, 16 heads of 64: forward 70 and 59, backward 154 and 148; ragged, dropped 44.7 and 43.8, 124.5 and
+//   121.  64 ragged sequences of up to 512, dropped: forward 97 in turn, 87 by one, 88 by two, 95 by eight; dQ 147, 133, 129, 135;
+//   dK and dV 146, 134, 132, 147: with eight or more, XCDs get unequal shares.
+// - 0 with fewer: 7 sequences of 1 to 1999 tokens, 4 key heads of 96: forward 74 in turn, 79 by one and 109 by two.
 struct Place { int unit, block; };   // (sequence, key head) and the workgroup's number among those of the unit
 __device__ __forceinline__ Place place(const SeqAttnArgs& a, int per_unit) {
-  const int id = blockIdx.x, units = a.sequences * a.kv_heads, eights = a.by_xcd ? units & ~7 : 0;
-  if (id < eights * per_unit) {
-    const int turn = id >> 3;
-    return Place{(turn / per_unit) * 8 + (id & 7), turn % per_unit};
+  const int id = blockIdx.x, run = a.xcd_run * per_unit;
+  if (a.xcd_run && id < a.sequences * a.kv_heads / (8 * a.xcd_run) * 8 * run) {
+    const int turn = id >> 3, at = turn % run;
+    return Place{((turn / run) * 8 + (id & 7)) * a.xcd_run + at / per_unit, at % per_unit};
   }
   return Place{id / per_unit, id % per_unit};
 }
@@ -450,37 +455,50 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
     }
   };
   if (tiles > 0) fetch(0);
-  if constexpr (WHOLE) {
-    const Tiles<E, DP> kt(a.k, sq.first, a.ldk, hk, n, a.d, wave, lane);
-    kt.fetch(0, lds0 + KIMG, wave);
-    if (n > CHA) kt.fetch(CHA, lds0 + KIMG + I::IMG, wave);
-  }
-  // WHOLE: -lse / scale and -D of the head's rows, two threads to a row (zeros past the sequence)
+  // WHOLE: -lse / scale and -D of the head's rows (zeros past the sequence), whole rows per load
   const auto head_stats = [&](int h) {
-    const int row = threadIdx.x >> 1, half = threadIdx.x & 1;
-    float D = 0.f, nl = 0.f;
-    if (row < n) {
-      const E* grow = (const E*)a.dout + (sq.first + row) * a.lddo + (long long)h * a.d;
-      const E* orow = (const E*)a.o + (sq.first + row) * a.ldo + (long long)h * a.d;
-#pragma unroll
-      for (int u = 0; u < DP / 16; ++u) {
-        const int col = (2 * u + half) * 8;
-        if (col < a.d) {
-          const typename Vec<E>::x8 gv = *(const typename Vec<E>::x8*)(grow + col), ov = *(const typename Vec<E>::x8*)(orow + col);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) D = fmaf(to_f32(gv[j]), to_f32(ov[j]), D);
-        }
-      }
-      nl = -a.lse[(long long)h * a.rows + sq.first + row] / a.scale;
-    }
-    D += dpp_move<0xB1>(D);   // the neighbour's half
+    constexpr int CH = DP / 8;   // lanes to a row
+    const int col = threadIdx.x % CH * 8;
     float* st = (float*)(lds + STAT + (h & 1) * 1024);
-    st[half * 128 + row] = half ? -D : nl;
+#pragma unroll
+    for (int u = 0; u < CH / 2; ++u) {
+      const int row = u * (256 / CH) + threadIdx.x / CH;
+      float D = 0.f;
+      if (row < n && col < a.d) {
+        const typename Vec<E>::x8 gv = *(const typename Vec<E>::x8*)((const E*)a.dout + (sq.first + row) * a.lddo + (long long)h * a.d + col);
+        const typename Vec<E>::x8 ov = *(const typename Vec<E>::x8*)((const E*)a.o + (sq.first + row) * a.ldo + (long long)h * a.d + col);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) D = fmaf(to_f32(gv[j]), to_f32(ov[j]), D);
+      }
+      D += dpp_move<0xB1>(D);
+      D += dpp_move<0x4E>(D);
+      if (CH == 8) D += dpp_move<0x141>(D);
+      if (col == 0) st[128 + row] = -D;
+    }
+    if (threadIdx.x < 128) st[threadIdx.x] = threadIdx.x < n ? -a.lse[(long long)h * a.rows + sq.first + threadIdx.x] / a.scale : 0.f;
   };
   const bool few = key0 == 0 && (a.causal || n <= 32);   // the wave's keys are all that the first 32 rows see
   bf16x8 kf[DP / 16], vf[DP / 16];
-  I::template row_frags<E>((const E*)a.k + (sq.first + kk) * a.ldk + (long long)hk * a.d, kk < n, a.d, lane, kf);
-  I::template row_frags<E>((const E*)a.v + (sq.first + kk) * a.ldv + (long long)hk * a.d, kk < n, a.d, lane, vf);
+  if constexpr (WHOLE) {   // through LDS, V where dS will be: loads of 16 bytes of 32 rows each are evicted and fetched again before the rows' other parts are read
+    const Tiles<E, DP> kt(a.k, sq.first, a.ldk, hk, n, a.d, wave, lane), vt(a.v, sq.first, a.ldv, hk, n, a.d, wave, lane);
+    kt.fetch(0, lds0 + KIMG, wave);
+    vt.fetch(0, lds0 + SIMG, wave);
+    if (n > CHA) {
+      kt.fetch(CHA, lds0 + KIMG + I::IMG, wave);
+      vt.fetch(CHA, lds0 + SIMG + I::IMG, wave);
+    }
+    head_stats(h0);
+    wait_vm0();
+    __syncthreads();
+#pragma unroll
+    for (int st = 0; st < DP / 16; ++st) {
+      kf[st] = I::rows_frag(lds + KIMG + (wave >> 1) * I::IMG, (wave & 1) * 32 + (lane & 31), st, lane);
+      vf[st] = I::rows_frag(lds + SIMG + (wave >> 1) * I::IMG, (wave & 1) * 32 + (lane & 31), st, lane);
+    }
+  } else {
+    I::template row_frags<E>((const E*)a.k + (sq.first + kk) * a.ldk + (long long)hk * a.d, kk < n, a.d, lane, kf);
+    I::template row_frags<E>((const E*)a.v + (sq.first + kk) * a.ldv + (long long)hk * a.d, kk < n, a.d, lane, vf);
+  }
   f32x16 dv[DP / 32], dk[DP / 32];
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t) { dv[t] = zero16(); dk[t] = zero16(); }
@@ -616,7 +634,7 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   for (int h = h0; i < tiles; ++h) {
     int t = h == h0 ? from % per_head : 0;
     const int end = min(per_head, t + tiles - i);
-    if (WHOLE) head_stats(h);
+    if (WHOLE && h != h0) head_stats(h);
     const auto grads = [&] {
       if constexpr (WHOLE) query_grads(h, (t0 + t) * CHA);
     };
