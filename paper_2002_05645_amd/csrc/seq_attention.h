@@ -281,7 +281,7 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
 
 // ---- dQ, and what the dK / dV kernel needs of each row ----------------------------------------------------------------
 template <typename E, int DP, bool DROP>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 32 ? 4 : DP <= 64 ? 3 : 2)))
 void seq_bwd_dq_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
   __shared__ __attribute__((aligned(1024))) char lds[4 * I::IMG];
@@ -335,6 +335,7 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t) dq[t] = zero16();
   const float c = a.scale * LOG2E, kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
+  const float nlc = nl * c;
   DropKey key;
   if (DROP) key = drop_key(a.seed, a.site, a.step);
   const auto arrive = [&](int t) {
@@ -349,15 +350,14 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
     const int lim = (a.causal ? min(n, q + 1) : n) - k0 - 4 * (lane >> 5);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      // the accumulators start from -lse / scale and -D instead of zero, which leaves one product each for P and dS
-      f32x16 s = splat16(nl), g = splat16(DROP ? 0.f : -D);
+      f32x16 s = zero16(), g = splat16(DROP ? 0.f : -D);   // (from -D instead of zero, which leaves one product for dS)
 #pragma unroll
       for (int st = 0; st < DP / 16; ++st) {
         s = mfma_32x32x16<E>(I::rows_frag(Ks, kb * 32 + (lane & 31), st, lane), qf[st], s);
         g = mfma_32x32x16<E>(I::rows_frag(Vs, kb * 32 + (lane & 31), st, lane), gf[st], g);
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * c);
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, nlc));
       if constexpr (decltype(edge)::value) {
 #pragma unroll
         for (int r = 0; r < 16; ++r)
