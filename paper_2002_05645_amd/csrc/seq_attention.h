@@ -157,7 +157,7 @@ __device__ __forceinline__ void store_part(const f32x16 (&acc)[DP / 32], float* 
 // A workgroup owns 128 NQ queries of one (sequence, head), each of its four waves 32 NQ of them, and walks the keys in tiles of 64; the next
 // tile's K and V are on their way into the other half of the LDS while one is computed.
 template <typename E, int DP, int NQ, bool DROP>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 64 ? 4 : 2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 64 ? 4 : DP <= 96 && DROP ? 3 : 2)))
 void seq_fwd_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
   __shared__ __attribute__((aligned(1024))) char lds[4 * I::IMG];
