@@ -43,6 +43,11 @@ DropGrid drop_grid(int rows, int n) {
   return g;
 }
 
+// Column sums of few rows: a workgroup to every eight columns, with a row to a thread, has all that goes into them, and the second kernel is
+// not run.  256 rows of 128 columns: 4.9 us instead of 4.1 + 2.5 and a launch; with four rows to a thread, 1024 of 1024, 8.0 against 4.9 + 2.9.
+constexpr int DROP_ONE_BLOCK_ROWS = 256;
+DropGrid drop_grid_one_block(int n) { return DropGrid{1, DROP_ONE_BLOCK_ROWS, (n + 7) / 8, 1, 1}; }
+
 // v[i] = v[i + by], 0 <= by < 8 (what comes from behind is not looked at)
 __device__ __forceinline__ void move_down(float (&v)[8], int by) {
 #pragma unroll
@@ -126,6 +131,23 @@ void dropout_kernel(const DropoutArgs a, int cw, int lanes, int groups, int per)
 #pragma unroll
     for (int i = 0; i < 8; ++i) red[threadIdx.x][i] = sums[i];
     __syncthreads();
+    if (a.rows <= DROP_ONE_BLOCK_ROWS) {   // all rows are here, of eight columns: 32 threads to a column, then one
+      __shared__ float red2[32][9];
+      const int i = threadIdx.x & 7, l0 = threadIdx.x >> 3;
+      float s = 0.f;
+#pragma unroll
+      for (int l = 0; l < 8; ++l) s += red[l0 + 32 * l][i];
+      red2[l0][i] = s;
+      __syncthreads();
+      if (threadIdx.x < 8 && group * 8 + i < a.n) {
+        const float old = a.accumulate ? a.dbias[group * 8 + i] : 0.f;
+        s = 0.f;
+#pragma unroll
+        for (int l = 0; l < 32; ++l) s += red2[l][i];
+        a.dbias[group * 8 + i] = old + s;
+      }
+      return;
+    }
     for (int u = threadIdx.x; u < cw * 8; u += 256) {
       const int c = u / 8, i = u % 8, to = (group * cw + c) * 8 + i;
       float s = 0.f;
@@ -164,7 +186,8 @@ __global__ __launch_bounds__(DROP_SUM_NT) void dropout_sum_kernel(const float* p
 
 template <typename T>
 void launch_dropout_t(const DropoutArgs& a, hipStream_t s) {
-  const DropGrid g = drop_grid(a.rows, a.n);
+  const bool one_block = a.dbias && a.rows <= DROP_ONE_BLOCK_ROWS;
+  const DropGrid g = one_block ? drop_grid_one_block(a.n) : drop_grid(a.rows, a.n);
   const dim3 grid((unsigned)((long long)g.groups * g.blocks));
   const auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a, g.cw, g.lanes, g.groups, g.per); };
   const auto rows = [&](auto resid, auto sums) {
@@ -176,7 +199,7 @@ void launch_dropout_t(const DropoutArgs& a, hipStream_t s) {
   };
   if (a.dbias) {
     rows(std::false_type{}, std::true_type{});
-    hipLaunchKernelGGL(dropout_sum_kernel, dim3((a.n + 15) / 16), dim3(DROP_SUM_NT), 0, s, a.part, g.blocks, a.n, a.dbias, a.accumulate);
+    if (!one_block) hipLaunchKernelGGL(dropout_sum_kernel, dim3((a.n + 15) / 16), dim3(DROP_SUM_NT), 0, s, a.part, g.blocks, a.n, a.dbias, a.accumulate);
   } else if (a.resid) {
     rows(std::true_type{}, std::false_type{});
   } else {
