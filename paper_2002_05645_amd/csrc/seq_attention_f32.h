@@ -4,6 +4,10 @@
 // the two halves (one 16-byte read feeds four instructions), and a product over the other tile's rows takes the rows 8 (r / 4) + r % 4
 // and those + 4 that accumulator register r holds in the two halves.
 // Bound by the fp32 matrix rate, a sixteenth of the 16-bit one: tiles of 32 rows, loaded through registers one tile ahead.
+// PARTS = 2, where the longest sequence has 33 to 64 rows: the waves that have no rows of the workgroup's 128 take every other tile of the
+// others' rows, and the two results are put together in LDS.  4 sequences of 64, 2 heads of 64, dropped: forward 9.0 -> 7.1 us,
+// dQ 12.3 -> 11.1, dK and dV 13.3 -> 10.6; 256 ragged ones, 12 heads: 56 -> 56, 89 -> 82, 103 -> 83.  (Of 32 or fewer rows there is one
+// tile, and the second buffers only cost: 34 -> 45, 54 -> 63, 62 -> 68.)
 #pragma once
 #include "seq_attention.h"
 
@@ -76,11 +80,19 @@ __device__ __forceinline__ void rows_f32(const float* img, const f32x16& p, f32x
     for (int t = 0; t < DP / 32; ++t) acc[t] = mfma_f32(ImgF<DP>::across(img, r, t, lane), p[r], acc[t]);
 }
 
-template <int DP, bool DROP>
+// the second part's accumulators (and what else each lane has) to the first: out by the waves with part = 1, in by their neighbours
+template <int N>
+__device__ __forceinline__ void give(float* to, const f32x16 (&acc)[N], int lane) {
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) to[(t * 16 + r) * 64 + lane] = acc[t][r];
+}
+
+template <int DP, bool DROP, int PARTS>
 __global__ __launch_bounds__(256) void seq_fwd_f32_kernel(const SeqAttnArgs a) {
   using I = ImgF<DP>;
-  __shared__ __attribute__((aligned(16))) float lds[2 * I::FLOATS];
-  float *Ks = lds, *Vs = lds + I::FLOATS;
+  __shared__ __attribute__((aligned(16))) float lds[PARTS * 2 * I::FLOATS];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
   const Place at = place(a, group * nblk);
   const int blk = nblk - 1 - at.block % nblk;
@@ -89,7 +101,7 @@ __global__ __launch_bounds__(256) void seq_fwd_f32_kernel(const SeqAttnArgs a) {
   const int n = sq.n, base_q = blk * 128;
   if (base_q >= n) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int q0 = base_q + wave * 32, q = q0 + (lane & 31);
+  const int part = wave / (4 / PARTS), q0 = base_q + wave % (4 / PARTS) * 32, q = q0 + (lane & 31);
   const bool active = q0 < n;
   const float* kb_ = (const float*)a.k + sq.first * a.ldk + (long long)hk * a.d;
   const float* vb_ = (const float*)a.v + sq.first * a.ldv + (long long)hk * a.d;
@@ -103,20 +115,28 @@ __global__ __launch_bounds__(256) void seq_fwd_f32_kernel(const SeqAttnArgs a) {
   const float c = a.scale * LOG2E;
   DropKey key;
   if (DROP) key = drop_key(a.seed, a.site, a.step);
-  I kr, vr;
-  kr.load(kb_, a.ldk, min(32, n), a.d);
-  vr.load(vb_, a.ldv, min(32, n), a.d);
-  for (int t = 0; t < tiles; ++t) {
-    __syncthreads();
-    kr.put(Ks);
-    vr.put(Vs);
-    __syncthreads();
-    const int k0 = t * 32;
-    if (t + 1 < tiles) {
-      kr.load(kb_ + (long long)(k0 + 32) * a.ldk, a.ldk, min(32, n - k0 - 32), a.d);
-      vr.load(vb_ + (long long)(k0 + 32) * a.ldv, a.ldv, min(32, n - k0 - 32), a.d);
+  I kr[PARTS], vr[PARTS];
+  const auto fetch = [&](int t) {
+#pragma unroll
+    for (int u = 0; u < PARTS; ++u) {
+      const int k0 = (t + u) * 32;   // (n - k0 <= 0: zeros)
+      kr[u].load(kb_ + (long long)k0 * a.ldk, a.ldk, n - k0, a.d);
+      vr[u].load(vb_ + (long long)k0 * a.ldv, a.ldv, n - k0, a.d);
     }
-    if (!active || (a.causal && k0 >= q0 + 32)) continue;
+  };
+  const float *Ks = lds + part * 2 * I::FLOATS, *Vs = Ks + I::FLOATS;   // this wave's of the tiles that are in
+  fetch(0);
+  for (int t = 0; t < tiles; t += PARTS) {
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < PARTS; ++u) {
+      kr[u].put(lds + u * 2 * I::FLOATS);
+      vr[u].put(lds + u * 2 * I::FLOATS + I::FLOATS);
+    }
+    __syncthreads();
+    if (t + PARTS < tiles) fetch(t + PARTS);
+    const int k0 = (t + part) * 32;
+    if (!active || t + part >= tiles || (a.causal && k0 >= q0 + 32)) continue;
     f32x16 s = zero16();
     columns_f32<DP>(Ks, qf, s, lane);
     if (k0 + 32 > n || (a.causal && k0 + 31 > q0)) {
@@ -148,6 +168,25 @@ __global__ __launch_bounds__(256) void seq_fwd_f32_kernel(const SeqAttnArgs a) {
     }
     rows_f32<DP>(Vs, s, o, lane);
   }
+  if (PARTS == 2) {   // (the first part has every row's first key)
+    float* mine = lds + (wave & 1) * (DP / 32 * 16 + 2) * 64;
+    __syncthreads();
+    if (part == 1) {
+      give(mine, o, lane);
+      mine[DP / 32 * 1024 + lane] = m;
+      mine[DP / 32 * 1024 + 64 + lane] = sum;
+    }
+    __syncthreads();
+    if (part == 1) return;
+    const float m2 = mine[DP / 32 * 1024 + lane], top = fmaxf(m, m2);
+    const float f = __builtin_amdgcn_exp2f((m - top) * c), f2 = __builtin_amdgcn_exp2f((m2 - top) * c);
+    sum = sum * f + mine[DP / 32 * 1024 + 64 + lane] * f2;
+    m = top;
+#pragma unroll
+    for (int t2 = 0; t2 < DP / 32; ++t2)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[t2][r] = o[t2][r] * f + mine[(t2 * 16 + r) * 64 + lane] * f2;
+  }
   if (!active) return;
   const float l = half_sum(sum), kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
   if (q >= n) return;
@@ -155,11 +194,10 @@ __global__ __launch_bounds__(256) void seq_fwd_f32_kernel(const SeqAttnArgs a) {
   if (a.lse && lane < 32) a.lse[(long long)h * a.rows + sq.first + q] = m * a.scale + __builtin_amdgcn_logf(l) * LN2;
 }
 
-template <int DP, bool DROP>
+template <int DP, bool DROP, int PARTS>
 __global__ __launch_bounds__(256) void seq_bwd_dq_f32_kernel(const SeqAttnArgs a) {
   using I = ImgF<DP>;
-  __shared__ __attribute__((aligned(16))) float lds[2 * I::FLOATS];
-  float *Ks = lds, *Vs = lds + I::FLOATS;
+  __shared__ __attribute__((aligned(16))) float lds[PARTS * 2 * I::FLOATS];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
   const Place at = place(a, group * nblk);
   const int blk = nblk - 1 - at.block % nblk;
@@ -168,7 +206,7 @@ __global__ __launch_bounds__(256) void seq_bwd_dq_f32_kernel(const SeqAttnArgs a
   const int n = sq.n, base_q = blk * 128;
   if (base_q >= n) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int q0 = base_q + wave * 32, q = q0 + (lane & 31);
+  const int part = wave / (4 / PARTS), q0 = base_q + wave % (4 / PARTS) * 32, q = q0 + (lane & 31);
   const bool active = q0 < n;
   const float* kb_ = (const float*)a.k + sq.first * a.ldk + (long long)hk * a.d;
   const float* vb_ = (const float*)a.v + sq.first * a.ldv + (long long)hk * a.d;
@@ -191,27 +229,35 @@ __global__ __launch_bounds__(256) void seq_bwd_dq_f32_kernel(const SeqAttnArgs a
     lse = a.lse[(long long)h * a.rows + sq.first + q];
   }
   D = half_sum(D);
-  if (q < n && lane < 32) a.delta[(long long)h * a.rows + sq.first + q] = D;
+  if (q < n && lane < 32 && part == 0) a.delta[(long long)h * a.rows + sq.first + q] = D;
   f32x16 dq[DP / 32];
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t) dq[t] = zero16();
   const float kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
   DropKey key;
   if (DROP) key = drop_key(a.seed, a.site, a.step);
-  I kr, vr;
-  kr.load(kb_, a.ldk, min(32, n), a.d);
-  vr.load(vb_, a.ldv, min(32, n), a.d);
-  for (int t = 0; t < tiles; ++t) {
-    __syncthreads();
-    kr.put(Ks);
-    vr.put(Vs);
-    __syncthreads();
-    const int k0 = t * 32;
-    if (t + 1 < tiles) {
-      kr.load(kb_ + (long long)(k0 + 32) * a.ldk, a.ldk, min(32, n - k0 - 32), a.d);
-      vr.load(vb_ + (long long)(k0 + 32) * a.ldv, a.ldv, min(32, n - k0 - 32), a.d);
+  I kr[PARTS], vr[PARTS];
+  const auto fetch = [&](int t) {
+#pragma unroll
+    for (int u = 0; u < PARTS; ++u) {
+      const int k0 = (t + u) * 32;   // (n - k0 <= 0: zeros)
+      kr[u].load(kb_ + (long long)k0 * a.ldk, a.ldk, n - k0, a.d);
+      vr[u].load(vb_ + (long long)k0 * a.ldv, a.ldv, n - k0, a.d);
     }
-    if (!active || (a.causal && k0 >= q0 + 32)) continue;
+  };
+  const float *Ks = lds + part * 2 * I::FLOATS, *Vs = Ks + I::FLOATS;   // this wave's of the tiles that are in
+  fetch(0);
+  for (int t = 0; t < tiles; t += PARTS) {
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < PARTS; ++u) {
+      kr[u].put(lds + u * 2 * I::FLOATS);
+      vr[u].put(lds + u * 2 * I::FLOATS + I::FLOATS);
+    }
+    __syncthreads();
+    if (t + PARTS < tiles) fetch(t + PARTS);
+    const int k0 = (t + part) * 32;
+    if (!active || t + part >= tiles || (a.causal && k0 >= q0 + 32)) continue;
     f32x16 s = zero16(), g = zero16();
     columns_f32<DP>(Ks, qf, s, lane);
     columns_f32<DP>(Vs, gf, g, lane);
@@ -226,15 +272,26 @@ __global__ __launch_bounds__(256) void seq_bwd_dq_f32_kernel(const SeqAttnArgs a
     }
     rows_f32<DP>(Ks, g, dq, lane);
   }
+  if (PARTS == 2) {
+    float* mine = lds + (wave & 1) * DP / 32 * 1024;
+    __syncthreads();
+    if (part == 1) give(mine, dq, lane);
+    __syncthreads();
+    if (part == 1) return;
+#pragma unroll
+    for (int t2 = 0; t2 < DP / 32; ++t2)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dq[t2][r] += mine[(t2 * 16 + r) * 64 + lane];
+  }
   if (!active || q >= n) return;
   I::store(dq, (float*)a.dq + (sq.first + q) * a.lddq + (long long)h * a.d, a.d, lane, a.scale);
 }
 
-template <int DP, bool DROP>
+template <int DP, bool DROP, int PARTS>
 __global__ __launch_bounds__(256) void seq_bwd_dkv_f32_kernel(const SeqAttnArgs a) {
   using I = ImgF<DP>;
-  __shared__ __attribute__((aligned(16))) float lds[2 * I::FLOATS + 64];
-  float *Qs = lds, *Gs = lds + I::FLOATS, *Ls = lds + 2 * I::FLOATS, *Ds = Ls + 32;
+  constexpr int STAGE = 2 * I::FLOATS + 64;   // Q, dO, and 32 rows' lse and D
+  __shared__ __attribute__((aligned(16))) float lds[PARTS * STAGE];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
   const Place at = place(a, nblk);
   const int blk = at.block, b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads;
@@ -242,19 +299,23 @@ __global__ __launch_bounds__(256) void seq_bwd_dkv_f32_kernel(const SeqAttnArgs 
   const int n = sq.n, base_k = blk * 128;
   if (base_k >= n) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int key0 = base_k + wave * 32, kk = key0 + (lane & 31);
+  const int part = wave / (4 / PARTS), key0 = base_k + wave % (4 / PARTS) * 32, kk = key0 + (lane & 31);
   const bool active = key0 < n;
   const int t0 = a.causal ? base_k / 32 : 0, per_head = (n + 31) / 32 - t0, tiles = per_head * group;
-  I qr, gr;
+  I qr[PARTS], gr[PARTS];
   float stat = 0.f;
   const auto fetch = [&](int i) {
-    const int h = hk * group + i / per_head, row0 = (t0 + i % per_head) * 32, rows = min(32, n - row0);
-    const long long tok = sq.first + row0;
-    qr.load((const float*)a.q + tok * a.ldq + (long long)h * a.d, a.ldq, rows, a.d);
-    gr.load((const float*)a.dout + tok * a.lddo + (long long)h * a.d, a.lddo, rows, a.d);
-    if (threadIdx.x < 64) {   // lse and D; rows past the sequence are zeros, which add nothing
-      const int row = threadIdx.x & 31;
-      stat = row < rows ? (threadIdx.x < 32 ? a.lse : a.delta)[(long long)h * a.rows + tok + row] : 0.f;
+#pragma unroll
+    for (int u = 0; u < PARTS; ++u) {
+      const bool live = i + u < tiles;
+      const int h = hk * group + (live ? (i + u) / per_head : 0), row0 = (t0 + (live ? (i + u) % per_head : 0)) * 32, rows = live ? n - row0 : 0;
+      const long long tok = sq.first + row0;
+      qr[u].load((const float*)a.q + tok * a.ldq + (long long)h * a.d, a.ldq, rows, a.d);
+      gr[u].load((const float*)a.dout + tok * a.lddo + (long long)h * a.d, a.lddo, rows, a.d);
+      if (threadIdx.x / 64 == u) {   // lse and D; rows past the sequence are zeros, which add nothing
+        const int row = threadIdx.x & 31;
+        stat = row < rows ? (lane < 32 ? a.lse : a.delta)[(long long)h * a.rows + tok + row] : 0.f;
+      }
     }
   };
   fetch(0);
@@ -267,15 +328,21 @@ __global__ __launch_bounds__(256) void seq_bwd_dkv_f32_kernel(const SeqAttnArgs 
   const float kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
   DropKey key;
   if (DROP) key = drop_key(a.seed, a.site, a.step);
-  for (int i = 0; i < tiles; ++i) {
+  const float *Qs = lds + part * STAGE, *Gs = Qs + I::FLOATS, *Ls = Gs + I::FLOATS, *Ds = Ls + 32;
+  for (int i0 = 0; i0 < tiles; i0 += PARTS) {
     __syncthreads();
-    qr.put(Qs);
-    gr.put(Gs);
-    if (threadIdx.x < 64) Ls[threadIdx.x] = stat;   // (Ds follows Ls)
+#pragma unroll
+    for (int u = 0; u < PARTS; ++u) {
+      qr[u].put(lds + u * STAGE);
+      gr[u].put(lds + u * STAGE + I::FLOATS);
+      if (threadIdx.x / 64 == u) lds[u * STAGE + 2 * I::FLOATS + lane] = stat;   // (Ds follows Ls)
+    }
     __syncthreads();
-    if (i + 1 < tiles) fetch(i + 1);
+    if (i0 + PARTS < tiles) fetch(i0 + PARTS);
+    const int i = i0 + part;
+    if (!active || i >= tiles) continue;
     const int h = hk * group + i / per_head, row0 = (t0 + i % per_head) * 32;
-    if (!active || (a.causal && row0 + 32 <= key0)) continue;
+    if (a.causal && row0 + 32 <= key0) continue;
     f32x16 s = zero16(), g = zero16();
     columns_f32<DP>(Qs, kf, s, lane);
     columns_f32<DP>(Gs, vf, g, lane);
@@ -294,6 +361,23 @@ __global__ __launch_bounds__(256) void seq_bwd_dkv_f32_kernel(const SeqAttnArgs 
     }
     rows_f32<DP>(Gs, s, dv, lane);
     rows_f32<DP>(Qs, g, dk, lane);
+  }
+  if (PARTS == 2) {
+    float* mine = lds + (wave & 1) * DP / 32 * 2048;
+    __syncthreads();
+    if (part == 1) {
+      give(mine, dv, lane);
+      give(mine + DP / 32 * 1024, dk, lane);
+    }
+    __syncthreads();
+    if (part == 1) return;
+#pragma unroll
+    for (int t2 = 0; t2 < DP / 32; ++t2)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        dv[t2][r] += mine[(t2 * 16 + r) * 64 + lane];
+        dk[t2][r] += mine[DP / 32 * 1024 + (t2 * 16 + r) * 64 + lane];
+      }
   }
   if (!active || kk >= n) return;
   I::store(dv, (float*)a.dv + (sq.first + kk) * a.lddv + (long long)hk * a.d, a.d, lane, kept);

@@ -37,12 +37,24 @@ void join(const SeqAttnArgs& a, const sattn::JoinArgs& j, hipStream_t s) {
 template <typename K>
 void go(K kern, dim3 grid, const SeqAttnArgs& a, hipStream_t s) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a); }
 
+#if L2L_ELEM == 0
+// dropped or not; waves without rows of their own on the others' tiles, where no sequence is longer than 64 (but the longest has two tiles)
+template <typename F>
+void pick_f32(const SeqAttnArgs& a, F f) {
+  typedef std::integral_constant<int, 1> One;
+  typedef std::integral_constant<int, 2> Two;
+  if (a.max_len > 32 && a.max_len <= 64) a.drop ? f(std::true_type{}, Two{}) : f(std::false_type{}, Two{});
+  else a.drop ? f(std::true_type{}, One{}) : f(std::false_type{}, One{});
+}
+#endif
+
 }  // namespace
 
 void L2L_NAME(l2l_seq_attn_fwd_)(const SeqAttnArgs& a, hipStream_t s) {
 #if L2L_ELEM == 0
-  if (a.drop) go(sattn::seq_fwd_f32_kernel<L2L_DP, true>, blocks(a, a.heads, 128), a, s);
-  else go(sattn::seq_fwd_f32_kernel<L2L_DP, false>, blocks(a, a.heads, 128), a, s);
+  pick_f32(a, [&](auto drop, auto parts) {
+    go(sattn::seq_fwd_f32_kernel<L2L_DP, decltype(drop)::value, decltype(parts)::value>, blocks(a, a.heads, 128), a, s);
+  });
 #else
   if (a.drop) go(sattn::seq_fwd_kernel<Elem, L2L_DP, 1, true>, blocks(a, a.heads * a.splits_fwd, 128), a, s);
   else go(sattn::seq_fwd_kernel<Elem, L2L_DP, 1, false>, blocks(a, a.heads * a.splits_fwd, 128), a, s);
@@ -53,13 +65,10 @@ void L2L_NAME(l2l_seq_attn_fwd_)(const SeqAttnArgs& a, hipStream_t s) {
 
 void L2L_NAME(l2l_seq_attn_bwd_)(const SeqAttnArgs& a, hipStream_t s) {
 #if L2L_ELEM == 0
-  if (a.drop) {
-    go(sattn::seq_bwd_dq_f32_kernel<L2L_DP, true>, blocks(a, a.heads, 128), a, s);
-    go(sattn::seq_bwd_dkv_f32_kernel<L2L_DP, true>, blocks(a, a.kv_heads, 128), a, s);
-  } else {
-    go(sattn::seq_bwd_dq_f32_kernel<L2L_DP, false>, blocks(a, a.heads, 128), a, s);
-    go(sattn::seq_bwd_dkv_f32_kernel<L2L_DP, false>, blocks(a, a.kv_heads, 128), a, s);
-  }
+  pick_f32(a, [&](auto drop, auto parts) {
+    go(sattn::seq_bwd_dq_f32_kernel<L2L_DP, decltype(drop)::value, decltype(parts)::value>, blocks(a, a.heads, 128), a, s);
+    go(sattn::seq_bwd_dkv_f32_kernel<L2L_DP, decltype(drop)::value, decltype(parts)::value>, blocks(a, a.kv_heads, 128), a, s);
+  });
 #else
   const auto both = [&](auto drop) {
     constexpr bool D = decltype(drop)::value;

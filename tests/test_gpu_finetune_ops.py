@@ -247,6 +247,19 @@ def test_attention_backward_in_one_kernel(ctx, dtype, heads, kv, d):
             x.check()
 
 
+@pytest.mark.parametrize("heads,kv,d", [(2, 2, 64), (4, 2, 24), (3, 1, 96), (2, 1, 128), (4, 4, 40)])
+def test_attention_short_fp32_sequences(ctx, heads, kv, d):
+    # no sequence beyond 64: two waves on a row block's tiles, and query tiles of several heads in turn
+    for causal in (False, True):
+        for p in (0.0, 0.3):
+            for lengths in ([64, 63, 33, 32, 31, 1, 0, 40], [20, 5], [64]):
+                x = Problem("fp32", heads, kv, d, lengths, causal, p, gaps=[0, 1] * 4, pad_cols=8, seed=d)
+                x.forward(ctx)
+                x.backward(ctx)
+                ctx.sync()
+                x.check()
+
+
 @pytest.mark.parametrize("dtype,d,longest", [("bf16", 64, 33), ("fp16", 32, 128), ("bf16", 96, 40), ("fp16", 128, 32), ("bf16", 64, 600)])
 @pytest.mark.parametrize("causal", [False, True])
 def test_attention_one_key_has_no_score_gradient(ctx, dtype, d, longest, causal):
