@@ -4,8 +4,8 @@
 // with Z the dropout factors (0 or 1 / kept share; dropout.h) and P taken again from S and lse in the backward pass, so
 // that nothing of size length^2 is stored.  Sequence b owns `len[b]` consecutive token rows from `first[b]` on; a query
 // sees the keys of its sequence, with `causal` those up to its own position.  Query head h reads key and value head
-// h / (heads / kv_heads); the gradients of a shared head are summed over its query heads in one workgroup's accumulators,
-// in a fixed order, so results do not depend on timing.
+// h / (heads / kv_heads); the gradients of a shared head are summed over its query heads in one workgroup's accumulators or in
+// several whose partial results a second kernel adds up, in a fixed order either way, so results do not depend on timing.
 //
 // Tiles, fragments and LDS images are those of attention.h: S^T = K Q^T with queries along the lanes in the forward and
 // dQ kernels, S = Q K^T with keys along the lanes in the dK / dV kernel, so that P and dS leave the accumulators as the B
@@ -154,26 +154,31 @@ __device__ __forceinline__ void store_part(const f32x16 (&acc)[DP / 32], float* 
 }
 
 // ---- forward -----------------------------------------------------------------------------------------------------------
-// A workgroup owns 128 NQ queries of one (sequence, head), each of its four waves 32 NQ of them, and walks the keys in tiles of 64; the next
-// tile's K and V are on their way into the other half of the LDS while one is computed.
-template <typename E, int DP, int NQ, bool DROP>
+// A workgroup owns 128 queries of one (sequence, head), each of its four waves 32 of them, and walks the keys in tiles of 64; the next
+// tile's K and V are on their way into the other half of the LDS while one is computed.  A tile's keys are taken in halves, which costs a second
+// look at the rows' maxima and saves 16 registers: a fourth wave a SIMD at 64 columns also with dropped probabilities.
+// Bound at 64 columns by vector instructions (109 of them, 16 exponentials, to 8 MFMA per wave and 32 keys; 62 % of the SIMDs' clocks at
+// three or more waves), at 128 by the matrix cores.  256 sequences of 128 tokens, 16 heads of 64: 60 us, 4.5 TB/s of the 5.1 that a copy
+// reaches; 64 of 512: 102 to 116 us.  One causal sequence of 16384, 32 heads on 8 of 128: 2200 to 2300 us, 970 TFLOP/s of the visible half
+// (a library product of 8192^3: 1221).
+template <typename E, int DP, bool DROP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 64 ? 4 : DP <= 96 && DROP ? 3 : 2)))
 void seq_fwd_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
   __shared__ __attribute__((aligned(1024))) char lds[4 * I::IMG];
-  const int nblk = (a.max_len + 128 * NQ - 1) / (128 * NQ), group = a.heads / a.kv_heads;
+  const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
   const Place at = place(a, group * nblk * a.splits_fwd);
   const int split = at.block % a.splits_fwd, of_head = at.block / a.splits_fwd;
   const int blk = nblk - 1 - of_head % nblk;   // (a causal sequence's longest blocks first)
   const int b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads, h = hk * group + of_head / nblk, bh = b * a.heads + h;
   const Seq sq = sequence(a, b);
-  const int n = sq.n, base_q = blk * 128 * NQ;
+  const int n = sq.n, base_q = blk * 128;
   if (base_q >= n) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int q0 = base_q + wave * 32 * NQ;
+  const int q0 = base_q + wave * 32, q = q0 + (lane & 31);
   const bool active = q0 < n;   // (per wave)
   const Tiles<E, DP> kt(a.k, sq.first, a.ldk, hk, n, a.d, wave, lane), vt(a.v, sq.first, a.ldv, hk, n, a.d, wave, lane);
-  const int last = a.causal ? min(n, base_q + 128 * NQ) : n, all_tiles = (last + CHA - 1) / CHA;
+  const int last = a.causal ? min(n, base_q + 128) : n, all_tiles = (last + CHA - 1) / CHA;
   const int from = all_tiles * split / a.splits_fwd, tiles = all_tiles * (split + 1) / a.splits_fwd;   // this split's
   const uint32_t lds0 = lds_place((const __attribute__((address_space(3))) char*)lds);
   const auto fetch = [&](int t) {
@@ -182,20 +187,14 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
     vt.fetch(t * CHA, to + I::IMG, wave);
   };
   if (from < tiles) fetch(from);
-  bf16x8 qf[NQ][DP / 16];
-  f32x16 o[NQ][DP / 32];
-  float m[NQ], sum[NQ];
-  // No row's maximum yet: far below any score, and finite, as a split's first tile may have no key that the row sees.
-  const float c = a.scale * LOG2E, lowest = fmaxf(-1e30f / c, -1e38f);
+  bf16x8 qf[DP / 16];
+  f32x16 o[DP / 32];
+  // No maximum yet: far below any score, and finite, as a split's first tile may have no key that the row sees.
+  const float c = a.scale * LOG2E;
+  float m = fmaxf(-1e30f / c, -1e38f), sum = 0.f;
+  I::template row_frags<E>((const E*)a.q + (sq.first + q) * a.ldq + (long long)h * a.d, q < n, a.d, lane, qf);
 #pragma unroll
-  for (int u = 0; u < NQ; ++u) {
-    const int q = q0 + u * 32 + (lane & 31);
-    I::template row_frags<E>((const E*)a.q + (sq.first + q) * a.ldq + (long long)h * a.d, q < n, a.d, lane, qf[u]);
-    m[u] = lowest;
-    sum[u] = 0.f;
-#pragma unroll
-    for (int t = 0; t < DP / 32; ++t) o[u][t] = zero16();
-  }
+  for (int t = 0; t < DP / 32; ++t) o[t] = zero16();
   DropKey key;
   if (DROP) key = drop_key(a.seed, a.site, a.step);
   const auto arrive = [&](int t) {
@@ -211,9 +210,9 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
     for (int kb = 0; kb < 2; ++kb) {
       f32x16 s = zero16();
 #pragma unroll
-      for (int st = 0; st < DP / 16; ++st) s = mfma_32x32x16<E>(I::rows_frag(Ks, kb * 32 + (lane & 31), st, lane), qf[0][st], s);
+      for (int st = 0; st < DP / 16; ++st) s = mfma_32x32x16<E>(I::rows_frag(Ks, kb * 32 + (lane & 31), st, lane), qf[st], s);
       if constexpr (decltype(edge)::value) {   // keys that a query does not see
-        const int q = q0 + (lane & 31), lim = (a.causal ? min(n, q + 1) : n) - k0 - 4 * (lane >> 5);
+        const int lim = (a.causal ? min(n, q + 1) : n) - k0 - 4 * (lane >> 5);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (kb * 32 + 8 * (r >> 2) + (r & 3) >= lim) s[r] = -INFINITY;
@@ -221,21 +220,21 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
       float cm = s[0];
 #pragma unroll
       for (int r = 1; r < 16; ++r) cm = fmaxf(cm, s[r]);
-      cm = fmaxf(half_max(cm), m[0]);
-      if (__any((cm - m[0]) * c > 8.0f)) {
-        const float rescale = __builtin_amdgcn_exp2f((m[0] - cm) * c);   // 0 on the first tile
-        m[0] = cm;
-        sum[0] *= rescale;
+      cm = fmaxf(half_max(cm), m);
+      if (__any((cm - m) * c > 8.0f)) {
+        const float rescale = __builtin_amdgcn_exp2f((m - cm) * c);   // 0 on the first tile
+        m = cm;
+        sum *= rescale;
 #pragma unroll
         for (int t2 = 0; t2 < DP / 32; ++t2)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) o[0][t2][r] *= rescale;
+          for (int r = 0; r < 16; ++r) o[t2][r] *= rescale;
       }
-      const float mc = m[0] * c;
+      const float mc = m * c;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -mc));
-        sum[0] += s[r];
+        sum += s[r];
       }
       if (DROP) {
         const u32x4 bytes = drop_bytes<true>(q0, k0 + kb * 32, (uint32_t)bh, key, lane);
@@ -246,14 +245,14 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
       for (int s2 = 0; s2 < 2; ++s2) {
         const bf16x8 pf = pack8<E>(s, 8 * s2);
 #pragma unroll
-        for (int t2 = 0; t2 < DP / 32; ++t2) o[0][t2] = mfma_32x32x16<E>(I::rows_T(Vs, kb, s2, t2, lane), pf, o[0][t2]);
+        for (int t2 = 0; t2 < DP / 32; ++t2) o[t2] = mfma_32x32x16<E>(I::rows_T(Vs, kb, s2, t2, lane), pf, o[t2]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   // The wave's tiles: those that all of its queries see whole, those with a mask, and those of its neighbours', where it only helps to
   // load.  In loops of their own: with the mask and the way round the work as branches inside one, the accumulators are copied back and forth.
-  const int mine = !active ? 0 : a.causal ? min(tiles, (q0 + 32 * NQ + CHA - 1) / CHA) : tiles;
+  const int mine = !active ? 0 : a.causal ? min(tiles, (q0 + 32 + CHA - 1) / CHA) : tiles;
   const int whole = min(mine, (a.causal ? min(n, q0 + 1) : n) / CHA);   // (counted from the first key, whatever the split)
   int t = from;
   for (; t < whole; ++t) { arrive(t); compute(t, std::false_type{}); }
@@ -262,24 +261,22 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
   __syncthreads();   // the images are no longer read: a quarter of them is each wave's way out
   if (!active) return;
   const float kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
-#pragma unroll
-  for (int u = 0; u < NQ; ++u) {
-    const int qr = q0 + u * 32, q = qr + (lane & 31);
-    if (qr >= n) break;
-    const float l = half_sum(sum[u]);
-    if (a.splits_fwd > 1) {   // (a split without a key that the row sees: l = 0)
-      const bool live = q < n, none = l == 0.f;
-      const long long row = (long long)split * a.rows + sq.first + q;
-      store_part<DP>(o[u], a.part + row * ((long long)a.heads * a.d) + (long long)h * a.d, live, a.d, lane, none ? 0.f : kept / l);
-      if (lane < 32 && live) a.part_lse[((long long)split * a.heads + h) * a.rows + sq.first + q] = none ? -INFINITY : (m[u] * c + __builtin_amdgcn_logf(l)) * LN2;
-      continue;
-    }
-    store_rows<E, DP>(o[u], lds + wave * I::IMG, (E*)a.out + (sq.first + qr) * a.ldo + (long long)h * a.d, a.ldo, n - qr, a.d, lane, kept / l);
-    if (a.lse && lane < 32 && q < n) a.lse[(long long)h * a.rows + sq.first + q] = (m[u] * c + __builtin_amdgcn_logf(l)) * LN2;
+  const float l = half_sum(sum);
+  if (a.splits_fwd > 1) {   // (a split without a key that the row sees: l = 0)
+    const bool none = l == 0.f;
+    const long long row = (long long)split * a.rows + sq.first + q;
+    store_part<DP>(o, a.part + row * ((long long)a.heads * a.d) + (long long)h * a.d, q < n, a.d, lane, none ? 0.f : kept / l);
+    if (lane < 32 && q < n) a.part_lse[((long long)split * a.heads + h) * a.rows + sq.first + q] = none ? -INFINITY : (m * c + __builtin_amdgcn_logf(l)) * LN2;
+    return;
   }
+  store_rows<E, DP>(o, lds + wave * I::IMG, (E*)a.out + (sq.first + q0) * a.ldo + (long long)h * a.d, a.ldo, n - q0, a.d, lane, kept / l);
+  if (a.lse && lane < 32 && q < n) a.lse[(long long)h * a.rows + sq.first + q] = (m * c + __builtin_amdgcn_logf(l)) * LN2;
 }
 
 // ---- dQ, and what the dK / dV kernel needs of each row ----------------------------------------------------------------
+// As the forward kernel, with dP beside S and dS K in the place of P V.  Bound by vector instructions and the latency of its three dependent
+// products at 64 columns (64 of 512 tokens, 16 heads: 163 us, 630 TFLOP/s; 124 us at two waves a SIMD and 114 at three with dropped
+// probabilities and ragged lengths), by the matrix cores at 128 (one causal sequence of 16384, 32 heads on 8: 2950 us, 1120 TFLOP/s).
 template <typename E, int DP, bool DROP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 32 ? 4 : DP <= 64 ? 3 : 2)))
 void seq_bwd_dq_kernel(const SeqAttnArgs a) {
@@ -415,7 +412,11 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
 // A workgroup owns 128 keys of one (sequence, key head) and walks the queries of all the head's query heads in tiles of 64.
 // WHOLE, where no sequence is longer than 128: the workgroup has all keys of its head, so that dQ of a tile can be made here as well, from dS
 // that the waves lay side by side in LDS, and the dQ kernel with its second pass over scores, probabilities and masks is not run.  The
-// rows' D and lse are taken from O, dO and lse at the head's start.
+// rows' D and lse are taken from O, dO and lse at the head's start.  (256 sequences of up to 128, 16 heads of 64, dropped: 119 us, the two
+// kernels 143; wider heads leave no registers for it.)
+// Bound at 64 columns by latency at two waves a SIMD (235 to 256 registers; at three they spill): 64 ragged sequences of up to 512, dropped,
+// 130 us; WHOLE by its first loads, half of a workgroup's life (256 of 128 tokens: 143 us, 3.7 TB/s), at 128 columns, one wave a SIMD,
+// by the matrix cores (one causal sequence of 16384, 32 heads on 8: 4600 us, 955 TFLOP/s).
 template <typename E, int DP, bool DROP, bool WHOLE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP > 96 ? 1 : 2)))
 void seq_bwd_dkv_kernel(const SeqAttnArgs a) {

@@ -56,8 +56,8 @@ void L2L_NAME(l2l_seq_attn_fwd_)(const SeqAttnArgs& a, hipStream_t s) {
     go(sattn::seq_fwd_f32_kernel<L2L_DP, decltype(drop)::value, decltype(parts)::value>, blocks(a, a.heads, 128), a, s);
   });
 #else
-  if (a.drop) go(sattn::seq_fwd_kernel<Elem, L2L_DP, 1, true>, blocks(a, a.heads * a.splits_fwd, 128), a, s);
-  else go(sattn::seq_fwd_kernel<Elem, L2L_DP, 1, false>, blocks(a, a.heads * a.splits_fwd, 128), a, s);
+  if (a.drop) go(sattn::seq_fwd_kernel<Elem, L2L_DP, true>, blocks(a, a.heads * a.splits_fwd, 128), a, s);
+  else go(sattn::seq_fwd_kernel<Elem, L2L_DP, false>, blocks(a, a.heads * a.splits_fwd, 128), a, s);
   if (a.splits_fwd > 1)
     join<true>(a, {{a.part}, a.rows * a.heads * a.d, a.part_lse, a.lse, {a.out}, {a.ldo}, a.splits_fwd, a.heads}, s);
 #endif
