@@ -2355,9 +2355,10 @@ static const char* attention_desc_error(const l2l_attention* a) {
 // `tiles`, and all `wgs` walks together are `total`; a compute unit takes its tiles one after the other, whichever of its workgroups they
 // belong to, so that the launch lasts as long as the longest walk, or as an even share and half a walk more.  Splits shorten the walk, up to
 // four workgroups a compute unit, and cost a launch and their fp32 partial results (`bytes` each).  Measured, whole and chosen splits
-// + their sum (us): one sequence of 2048, 4 query heads on 1 of 64 columns, dropped: forward 40, 18 + 10; dQ 47, 20 + 5; dK and dV
-// 206, 29 + 8.  Two of 1024, 16 heads on 4 of 128: dK and dV 138, 63 + 10; its forward stays whole at 29 (two splits: 31 + 13).  A causal
-// 16384, 32 heads on 8 of 128, stays whole: dK and dV 4520 (two splits: 4445 + 93).
+// + their sum (us): one sequence of 2048, 4 query heads on 1 of 64 columns, dropped: forward 40, 19 + 8; dQ 47, 24 + 7; dK and dV
+// 206, 30 + 7.  Two of 1024, 16 heads on 4 of 128: dK and dV 138, 63 + 10; its forward stays whole at 29 (two splits: 31 + 13).  A causal
+// 16384, 32 heads on 8 of 128, stays whole: dK and dV 4520 (two splits: 4445 + 93).  fp32, one causal sequence of
+// 2048, 2 heads on 1 of 128: forward 299, 48 + 16; dQ 401, 59 + 16; dK and dV 1066, 84 + 16.
 static int attention_splits(double wgs, int tiles, double total, double us_per_tile, double bytes) {
   int best_s = 1;
   double best = 1e300;
@@ -2374,13 +2375,14 @@ static AttentionSplits attention_plan(const l2l_attention* a) {
   AttentionSplits p = {1, 1, 1, 0, 0};
   const double rows = (double)a->rows, q = rows * a->heads, kv = rows * a->kv_heads;
   const size_t stats = ((size_t)(2 * q) * 4 + 15) / 16 * 16;
-  if (is16(a->dtype) && a->max_len > 0) {
+  if (a->max_len > 0 && a->sequences > 0) {
     // How long the sequences really are only the device knows: max_len and the token rows bound them.
     const int tiles = (a->max_len + 63) / 64, group = a->heads / a->kv_heads;
     const double len = std::min((double)a->max_len, rows / a->sequences);
     const double blocks = std::min(rows / 128 + a->sequences, (double)a->sequences * ((a->max_len + 127) / 128));
     const double total = blocks * len / 64 * a->heads * (a->causal ? 0.5 : 1.0);
-    const double us = std::max(0.8, a->head_dim / 60.0) + (a->dropout > 0 ? 0.7 : 0.0);   // of a tile (1.1 at 64 columns, 2.1 at 128; 1.8 and 2.4 at 64 and 96 dropped)
+    // of a tile (16-bit formats: 1.1 us at 64 columns, 2.1 at 128, 1.8 and 2.4 at 64 and 96 dropped; fp32: 3.4 to 7.2 at 64)
+    const double us = is16(a->dtype) ? std::max(0.8, a->head_dim / 60.0) + (a->dropout > 0 ? 0.7 : 0.0) : std::max(2.0, a->head_dim / 13.0);
     p.fwd = p.dq = attention_splits(blocks * a->heads, tiles, total, us, q * a->head_dim * 4);
     p.dkv = attention_splits(blocks * a->kv_heads, tiles * group, total, us, 2 * kv * a->head_dim * 4);
   }

@@ -19,7 +19,7 @@ struct SeqAttnArgs {
   uint32_t drop;                      // of 256; 0 = no dropout
   uint64_t seed, site;
   const uint64_t* step;
-  // Splits over the long axis (16-bit formats): of a query block's keys (forward, dQ) and of a key block's queries and query
+  // Splits over the long axis: of a query block's keys (forward, dQ) and of a key block's queries and query
   // heads (dK / dV).  Above 1 the kernels leave fp32 partial results that a second kernel adds up.
   int splits_fwd, splits_dq, splits_dkv;
   float* part;                        // [split][rows][heads d]; dK / dV: [split][2][rows][kv_heads d], dV first

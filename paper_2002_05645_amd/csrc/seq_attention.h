@@ -680,22 +680,34 @@ __global__ __launch_bounds__(256) void seq_join_kernel(const SeqAttnArgs a, cons
     const int i = blk * 64 + u / chunks, col = u % chunks * 8;
     if (i >= sq.n) return;
     const long long row = sq.first + i, at = row * ((long long)j.heads * a.d) + (long long)h * a.d + col;
+    // four splits' loads at a time, without a branch between them: places past the last split are read again and count nothing
     float top = -INFINITY, total = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const auto lse_of = [&](int s) { return j.part_lse[((long long)min(s, j.splits - 1) * j.heads + h) * a.rows + row]; };
     if (WEIGHTED) {
-      for (int s = 0; s < j.splits; ++s) top = fmaxf(top, j.part_lse[((long long)s * j.heads + h) * a.rows + row]);
-    }
-    for (int s = 0; s < j.splits; ++s) {
-      float w = 1.f;
-      if (WEIGHTED) {
-        const float l = j.part_lse[((long long)s * j.heads + h) * a.rows + row];
-        if (l == -INFINITY) continue;   // (nothing was stored)
-        w = __builtin_amdgcn_exp2f((l - top) * LOG2E);
-        total += w;
-      }
-      float v[8];
-      load8(part + s * j.split_stride + at, v);
+      for (int s0 = 0; s0 < j.splits; s0 += 4) {
+        float l[4];
 #pragma unroll
-      for (int x = 0; x < 8; ++x) acc[x] = fmaf(v[x], w, acc[x]);
+        for (int x = 0; x < 4; ++x) l[x] = lse_of(s0 + x);
+        top = fmaxf(fmaxf(top, fmaxf(l[0], l[1])), fmaxf(l[2], l[3]));
+      }
+    }
+    for (int s0 = 0; s0 < j.splits; s0 += 4) {
+      float v[4][8], w[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        load8(part + min(s0 + x, j.splits - 1) * j.split_stride + at, v[x]);
+        w[x] = WEIGHTED ? lse_of(s0 + x) : 0.f;
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if (s0 + x >= j.splits) continue;
+        if (WEIGHTED) {
+          w[x] = w[x] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((w[x] - top) * LOG2E);   // (-inf: a split without a key that the row sees)
+          total += w[x];
+        }
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[c] = WEIGHTED ? fmaf(v[x][c], w[x], acc[c]) : acc[c] + v[x][c];
+      }
     }
     if (WEIGHTED) {
 #pragma unroll

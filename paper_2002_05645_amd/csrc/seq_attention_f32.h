@@ -94,9 +94,9 @@ __global__ __launch_bounds__(256) void seq_fwd_f32_kernel(const SeqAttnArgs a) {
   using I = ImgF<DP>;
   __shared__ __attribute__((aligned(16))) float lds[PARTS * 2 * I::FLOATS];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, group * nblk);
-  const int blk = nblk - 1 - at.block % nblk;
-  const int b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads, h = hk * group + at.block / nblk, bh = b * a.heads + h;
+  const Place at = place(a, group * nblk * a.splits_fwd);
+  const int split = at.block % a.splits_fwd, of_head = at.block / a.splits_fwd, blk = nblk - 1 - of_head % nblk;
+  const int b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads, h = hk * group + of_head / nblk, bh = b * a.heads + h;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_q = blk * 128;
   if (base_q >= n) return;
@@ -105,7 +105,8 @@ __global__ __launch_bounds__(256) void seq_fwd_f32_kernel(const SeqAttnArgs a) {
   const bool active = q0 < n;
   const float* kb_ = (const float*)a.k + sq.first * a.ldk + (long long)hk * a.d;
   const float* vb_ = (const float*)a.v + sq.first * a.ldv + (long long)hk * a.d;
-  const int last = a.causal ? min(n, base_q + 128) : n, tiles = (last + 31) / 32;
+  const int last = a.causal ? min(n, base_q + 128) : n, all_tiles = (last + 31) / 32;
+  const int from = all_tiles * split / a.splits_fwd, tiles = all_tiles * (split + 1) / a.splits_fwd;
   f32x4 qf[DP / 8];
   I::row((const float*)a.q + (sq.first + q) * a.ldq + (long long)h * a.d, q < n, a.d, lane, qf);
   f32x16 o[DP / 32];
@@ -125,8 +126,8 @@ __global__ __launch_bounds__(256) void seq_fwd_f32_kernel(const SeqAttnArgs a) {
     }
   };
   const float *Ks = lds + part * 2 * I::FLOATS, *Vs = Ks + I::FLOATS;   // this wave's of the tiles that are in
-  fetch(0);
-  for (int t = 0; t < tiles; t += PARTS) {
+  fetch(from);
+  for (int t = from; t < tiles; t += PARTS) {
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < PARTS; ++u) {
@@ -190,6 +191,13 @@ __global__ __launch_bounds__(256) void seq_fwd_f32_kernel(const SeqAttnArgs a) {
   if (!active) return;
   const float l = half_sum(sum), kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
   if (q >= n) return;
+  if (a.splits_fwd > 1) {   // (a split without a key that the row sees: l = 0)
+    const bool none = l == 0.f;
+    const long long row = (long long)split * a.rows + sq.first + q;
+    I::store(o, a.part + row * ((long long)a.heads * a.d) + (long long)h * a.d, a.d, lane, none ? 0.f : kept / l);
+    if (lane < 32) a.part_lse[((long long)split * a.heads + h) * a.rows + sq.first + q] = none ? -INFINITY : m * a.scale + __builtin_amdgcn_logf(l) * LN2;
+    return;
+  }
   I::store(o, (float*)a.out + (sq.first + q) * a.ldo + (long long)h * a.d, a.d, lane, kept / l);
   if (a.lse && lane < 32) a.lse[(long long)h * a.rows + sq.first + q] = m * a.scale + __builtin_amdgcn_logf(l) * LN2;
 }
@@ -199,9 +207,9 @@ __global__ __launch_bounds__(256) void seq_bwd_dq_f32_kernel(const SeqAttnArgs a
   using I = ImgF<DP>;
   __shared__ __attribute__((aligned(16))) float lds[PARTS * 2 * I::FLOATS];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, group * nblk);
-  const int blk = nblk - 1 - at.block % nblk;
-  const int b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads, h = hk * group + at.block / nblk, bh = b * a.heads + h;
+  const Place at = place(a, group * nblk * a.splits_dq);
+  const int split = at.block % a.splits_dq, of_head = at.block / a.splits_dq, blk = nblk - 1 - of_head % nblk;
+  const int b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads, h = hk * group + of_head / nblk, bh = b * a.heads + h;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_q = blk * 128;
   if (base_q >= n) return;
@@ -210,7 +218,8 @@ __global__ __launch_bounds__(256) void seq_bwd_dq_f32_kernel(const SeqAttnArgs a
   const bool active = q0 < n;
   const float* kb_ = (const float*)a.k + sq.first * a.ldk + (long long)hk * a.d;
   const float* vb_ = (const float*)a.v + sq.first * a.ldv + (long long)hk * a.d;
-  const int last = a.causal ? min(n, base_q + 128) : n, tiles = (last + 31) / 32;
+  const int last = a.causal ? min(n, base_q + 128) : n, all_tiles = (last + 31) / 32;
+  const int from = all_tiles * split / a.splits_dq, tiles = all_tiles * (split + 1) / a.splits_dq;
   f32x4 qf[DP / 8], gf[DP / 8];
   const float* orow = (const float*)a.o + (sq.first + q) * a.ldo + (long long)h * a.d;
   I::row((const float*)a.q + (sq.first + q) * a.ldq + (long long)h * a.d, q < n, a.d, lane, qf);
@@ -229,7 +238,7 @@ __global__ __launch_bounds__(256) void seq_bwd_dq_f32_kernel(const SeqAttnArgs a
     lse = a.lse[(long long)h * a.rows + sq.first + q];
   }
   D = half_sum(D);
-  if (q < n && lane < 32 && part == 0) a.delta[(long long)h * a.rows + sq.first + q] = D;
+  if (q < n && lane < 32 && part == 0 && split == 0) a.delta[(long long)h * a.rows + sq.first + q] = D;
   f32x16 dq[DP / 32];
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t) dq[t] = zero16();
@@ -246,8 +255,8 @@ __global__ __launch_bounds__(256) void seq_bwd_dq_f32_kernel(const SeqAttnArgs a
     }
   };
   const float *Ks = lds + part * 2 * I::FLOATS, *Vs = Ks + I::FLOATS;   // this wave's of the tiles that are in
-  fetch(0);
-  for (int t = 0; t < tiles; t += PARTS) {
+  fetch(from);
+  for (int t = from; t < tiles; t += PARTS) {
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < PARTS; ++u) {
@@ -284,6 +293,11 @@ __global__ __launch_bounds__(256) void seq_bwd_dq_f32_kernel(const SeqAttnArgs a
       for (int r = 0; r < 16; ++r) dq[t2][r] += mine[(t2 * 16 + r) * 64 + lane];
   }
   if (!active || q >= n) return;
+  if (a.splits_dq > 1) {
+    const long long row = (long long)split * a.rows + sq.first + q;
+    I::store(dq, a.part + row * ((long long)a.heads * a.d) + (long long)h * a.d, a.d, lane, a.scale);
+    return;
+  }
   I::store(dq, (float*)a.dq + (sq.first + q) * a.lddq + (long long)h * a.d, a.d, lane, a.scale);
 }
 
@@ -293,15 +307,16 @@ __global__ __launch_bounds__(256) void seq_bwd_dkv_f32_kernel(const SeqAttnArgs 
   constexpr int STAGE = 2 * I::FLOATS + 64;   // Q, dO, and 32 rows' lse and D
   __shared__ __attribute__((aligned(16))) float lds[PARTS * STAGE];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, nblk);
-  const int blk = at.block, b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads;
+  const Place at = place(a, nblk * a.splits_dkv);
+  const int split = at.block % a.splits_dkv, blk = at.block / a.splits_dkv, b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_k = blk * 128;
   if (base_k >= n) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int part = wave / (4 / PARTS), key0 = base_k + wave % (4 / PARTS) * 32, kk = key0 + (lane & 31);
   const bool active = key0 < n;
-  const int t0 = a.causal ? base_k / 32 : 0, per_head = (n + 31) / 32 - t0, tiles = per_head * group;
+  const int t0 = a.causal ? base_k / 32 : 0, per_head = (n + 31) / 32 - t0, all_tiles = per_head * group;
+  const int from = all_tiles * split / a.splits_dkv, tiles = all_tiles * (split + 1) / a.splits_dkv;   // this split's, of all heads' in turn
   I qr[PARTS], gr[PARTS];
   float stat = 0.f;
   const auto fetch = [&](int i) {
@@ -318,7 +333,7 @@ __global__ __launch_bounds__(256) void seq_bwd_dkv_f32_kernel(const SeqAttnArgs 
       }
     }
   };
-  fetch(0);
+  fetch(from);
   f32x4 kf[DP / 8], vf[DP / 8];
   I::row((const float*)a.k + (sq.first + kk) * a.ldk + (long long)hk * a.d, kk < n, a.d, lane, kf);
   I::row((const float*)a.v + (sq.first + kk) * a.ldv + (long long)hk * a.d, kk < n, a.d, lane, vf);
@@ -329,7 +344,7 @@ __global__ __launch_bounds__(256) void seq_bwd_dkv_f32_kernel(const SeqAttnArgs 
   DropKey key;
   if (DROP) key = drop_key(a.seed, a.site, a.step);
   const float *Qs = lds + part * STAGE, *Gs = Qs + I::FLOATS, *Ls = Gs + I::FLOATS, *Ds = Ls + 32;
-  for (int i0 = 0; i0 < tiles; i0 += PARTS) {
+  for (int i0 = from; i0 < tiles; i0 += PARTS) {
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < PARTS; ++u) {
@@ -380,6 +395,12 @@ __global__ __launch_bounds__(256) void seq_bwd_dkv_f32_kernel(const SeqAttnArgs 
       }
   }
   if (!active || kk >= n) return;
+  if (a.splits_dkv > 1) {
+    const long long width = (long long)a.kv_heads * a.d, row = 2LL * split * a.rows + sq.first + kk;
+    I::store(dv, a.part + row * width + (long long)hk * a.d, a.d, lane, kept);
+    I::store(dk, a.part + (row + a.rows) * width + (long long)hk * a.d, a.d, lane, a.scale);
+    return;
+  }
   I::store(dv, (float*)a.dv + (sq.first + kk) * a.lddv + (long long)hk * a.d, a.d, lane, kept);
   I::store(dk, (float*)a.dk + (sq.first + kk) * a.lddk + (long long)hk * a.d, a.d, lane, a.scale);
 }

@@ -26,13 +26,23 @@ dim3 blocks(const SeqAttnArgs& a, int heads, int rows_per) {
   return dim3((unsigned)((long long)a.sequences * heads * ((a.max_len + rows_per - 1) / rows_per)));
 }
 
-#if L2L_ELEM != 0
+// the splits' partial results together, where there are any
 template <bool WEIGHTED>
 void join(const SeqAttnArgs& a, const sattn::JoinArgs& j, hipStream_t s) {
   const dim3 grid((unsigned)((long long)a.sequences * j.heads * ((a.max_len + 63) / 64)), j.out[1] ? 2 : 1);
   hipLaunchKernelGGL((sattn::seq_join_kernel<Elem, WEIGHTED>), grid, dim3(256), 0, s, a, j);
 }
-#endif
+void join_fwd(const SeqAttnArgs& a, hipStream_t s) {
+  if (a.splits_fwd > 1) join<true>(a, {{a.part}, a.rows * a.heads * a.d, a.part_lse, a.lse, {a.out}, {a.ldo}, a.splits_fwd, a.heads}, s);
+}
+void join_dq(const SeqAttnArgs& a, hipStream_t s) {
+  if (a.splits_dq > 1) join<false>(a, {{a.part}, a.rows * a.heads * a.d, nullptr, nullptr, {a.dq}, {a.lddq}, a.splits_dq, a.heads}, s);
+}
+void join_dkv(const SeqAttnArgs& a, hipStream_t s) {
+  const long long one = a.rows * a.kv_heads * a.d;
+  if (a.splits_dkv > 1)
+    join<false>(a, {{a.part, a.part + one}, 2 * one, nullptr, nullptr, {a.dv, a.dk}, {a.lddv, a.lddk}, a.splits_dkv, a.kv_heads}, s);
+}
 
 template <typename K>
 void go(K kern, dim3 grid, const SeqAttnArgs& a, hipStream_t s) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a); }
@@ -53,21 +63,22 @@ void pick_f32(const SeqAttnArgs& a, F f) {
 void L2L_NAME(l2l_seq_attn_fwd_)(const SeqAttnArgs& a, hipStream_t s) {
 #if L2L_ELEM == 0
   pick_f32(a, [&](auto drop, auto parts) {
-    go(sattn::seq_fwd_f32_kernel<L2L_DP, decltype(drop)::value, decltype(parts)::value>, blocks(a, a.heads, 128), a, s);
+    go(sattn::seq_fwd_f32_kernel<L2L_DP, decltype(drop)::value, decltype(parts)::value>, blocks(a, a.heads * a.splits_fwd, 128), a, s);
   });
 #else
   if (a.drop) go(sattn::seq_fwd_kernel<Elem, L2L_DP, true>, blocks(a, a.heads * a.splits_fwd, 128), a, s);
   else go(sattn::seq_fwd_kernel<Elem, L2L_DP, false>, blocks(a, a.heads * a.splits_fwd, 128), a, s);
-  if (a.splits_fwd > 1)
-    join<true>(a, {{a.part}, a.rows * a.heads * a.d, a.part_lse, a.lse, {a.out}, {a.ldo}, a.splits_fwd, a.heads}, s);
 #endif
+  join_fwd(a, s);
 }
 
 void L2L_NAME(l2l_seq_attn_bwd_)(const SeqAttnArgs& a, hipStream_t s) {
 #if L2L_ELEM == 0
   pick_f32(a, [&](auto drop, auto parts) {
-    go(sattn::seq_bwd_dq_f32_kernel<L2L_DP, decltype(drop)::value, decltype(parts)::value>, blocks(a, a.heads, 128), a, s);
-    go(sattn::seq_bwd_dkv_f32_kernel<L2L_DP, decltype(drop)::value, decltype(parts)::value>, blocks(a, a.kv_heads, 128), a, s);
+    go(sattn::seq_bwd_dq_f32_kernel<L2L_DP, decltype(drop)::value, decltype(parts)::value>, blocks(a, a.heads * a.splits_dq, 128), a, s);
+    join_dq(a, s);
+    go(sattn::seq_bwd_dkv_f32_kernel<L2L_DP, decltype(drop)::value, decltype(parts)::value>, blocks(a, a.kv_heads * a.splits_dkv, 128), a, s);
+    join_dkv(a, s);
   });
 #else
   const auto both = [&](auto drop) {
@@ -80,12 +91,9 @@ void L2L_NAME(l2l_seq_attn_bwd_)(const SeqAttnArgs& a, hipStream_t s) {
     }
     {
       go(sattn::seq_bwd_dq_kernel<Elem, L2L_DP, D>, blocks(a, a.heads * a.splits_dq, 128), a, s);
-      if (a.splits_dq > 1) join<false>(a, {{a.part}, a.rows * a.heads * a.d, nullptr, nullptr, {a.dq}, {a.lddq}, a.splits_dq, a.heads}, s);
+      join_dq(a, s);
       go(sattn::seq_bwd_dkv_kernel<Elem, L2L_DP, D, false>, blocks(a, a.kv_heads * a.splits_dkv, 128), a, s);
-      if (a.splits_dkv > 1) {
-        const long long one = a.rows * a.kv_heads * a.d;
-        join<false>(a, {{a.part, a.part + one}, 2 * one, nullptr, nullptr, {a.dv, a.dk}, {a.lddv, a.lddk}, a.splits_dkv, a.kv_heads}, s);
-      }
+      join_dkv(a, s);
     }
   };
   if (a.drop) both(std::true_type{});

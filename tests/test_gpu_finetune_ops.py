@@ -212,7 +212,8 @@ def test_attention_rows_far_behind_32_bit_offsets(ctx):
 
 
 @pytest.mark.parametrize("causal", [False, True])
-@pytest.mark.parametrize("dtype,heads,kv,d", [("bf16", 4, 1, 64), ("fp16", 3, 3, 96), ("bf16", 2, 2, 32), ("fp16", 4, 2, 128), ("bf16", 3, 1, 40), ("fp16", 1, 1, 8)])
+@pytest.mark.parametrize("dtype,heads,kv,d", [("bf16", 4, 1, 64), ("fp16", 3, 3, 96), ("bf16", 2, 2, 32), ("fp16", 4, 2, 128), ("bf16", 3, 1, 40), ("fp16", 1, 1, 8), ("fp32", 4, 1, 64), ("fp32", 2, 2, 128),
+                                              ("fp32", 3, 1, 24)])
 def test_attention_few_workgroups_share_the_long_axis(ctx, dtype, heads, kv, d, causal):
     # so few (sequence, head, block)s that the workgroups take parts of the keys, or of the queries, and a second kernel adds them up; splits that end
     # in the middle of a causal row, and short sequences whose splits are empty
@@ -223,6 +224,18 @@ def test_attention_few_workgroups_share_the_long_axis(ctx, dtype, heads, kv, d, 
         x.backward(ctx)
         ctx.sync()
         x.check()
+
+
+def test_attention_fp32_gradients_of_shared_heads_in_parts(ctx):
+    # two waves on a tile pair, and parts that begin and end in the middle of a head's tiles
+    for lengths in ([64, 40], [33, 64, 1, 0]):
+        for causal in (False, True):
+            x = Problem("fp32", 14, 2, 64, lengths, causal, 0.2, seed=14)
+            assert x.work.numel() >= 14 * x.rows * 8 + 2 * 2 * 2 * x.rows * 64 * 4
+            x.forward(ctx)
+            x.backward(ctx)
+            ctx.sync()
+            x.check()
 
 
 def test_attention_forward_without_workspace_is_not_split(ctx):
