@@ -357,7 +357,7 @@ typedef struct {
   const int32_t* first;
   const int32_t* len;
   int causal;            /* 1: a query sees the keys up to its own position; 0: all of its sequence */
-  float scale;           /* > 0: factor on the scores, 1 / sqrt(d) as a rule */
+  float scale;           /* 2^-64 to 2^64: factor on the scores, 1 / sqrt(d) as a rule */
   double dropout;        /* share of the probabilities that is dropped (the others are divided by the kept share); to the
                             nearest 1/256, one random byte a probability: byte 4 (i % 4) + j % 4 of the call with counter words 0, 1 =
                             (i / 4) << 16 | j / 4, 2^31 | (b heads + h) for query i, key j of sequence b and head h is kept if >= 256 p */
@@ -367,7 +367,8 @@ typedef struct {
 /* o = (softmax(scale q k^T) dropped) v.  q, o: [rows, heads d], k, v: [rows, kv_heads d], each with its own row stride in elements (column
    groups of one QKV matrix do); 16-byte aligned, strides too.  lse: float [heads][rows], the logarithm of each softmax
    row's denominator (NULL: not wanted; the backward call needs it).  work: l2l_op_attention_work_bytes bytes, 16-byte aligned, or NULL,
-   which leaves every row's keys to one workgroup also where there are few rows. */
+   which leaves every row's keys to one workgroup also where there are few rows.  (How many parts a row is added up
+   from follows from the sizes in the description: its last bits may differ between batches.) */
 int l2l_op_attention(l2l_ctx*, const l2l_attention*, const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv,
                      void* o, long long ldo, float* lse, void* work);
 /* Its gradients: dq [rows, heads d], dk, dv [rows, kv_heads d] (summed over the query heads that share them) from dout, the
@@ -380,13 +381,13 @@ int l2l_op_attention_bwd(l2l_ctx*, const l2l_attention*, const void* q, long lon
 size_t l2l_op_attention_work_bytes(const l2l_attention*);
 
 /* y = resid + drop(x + bias), [rows, n] with row strides in elements of any alignment; bias [n] and resid may be NULL; in
-   place (y = x or y = resid, same stride) allowed.  p: share of the elements that is dropped (the others are divided by
+   place (y = x or y = resid, same stride) allowed; rows and n at most 2^30.  p: share of the elements that is dropped (the others are divided by
    the kept share), to the nearest 1/65536: 16 random bits an element, half-word j % 8 (low half of word 0 first) of the call with
    counter words 0, 1 = j / 8, i for element (i, j), kept if >= 65536 p. */
 int l2l_op_dropout(l2l_ctx*, int dtype, int rows, int n, const void* x, long long ldx, const void* bias, const void* resid, long long ldr,
                    void* y, long long ldy, double p, uint64_t seed, uint64_t site, const uint64_t* step);
 /* dx = drop(dy) with the forward call's p, seed, site and step (the gradient of x; that of resid is dy).  dbias: float [n] or NULL,
-   receives the column sums of dx before their rounding (accumulate = 1: they are added to it); it needs work: l2l_op_dropout_work_bytes
+   receives the column sums of dx before their rounding (accumulate = 1: they are added to it; n at most 2^25); it needs work: l2l_op_dropout_work_bytes
    bytes, 16-byte aligned.  In place allowed. */
 int l2l_op_dropout_bwd(l2l_ctx*, int dtype, int rows, int n, const void* dy, long long lddy, void* dx, long long lddx, double p, uint64_t seed,
                        uint64_t site, const uint64_t* step, float* dbias, int accumulate, void* work);
@@ -397,7 +398,7 @@ size_t l2l_op_dropout_work_bytes(int rows, int n);
    = log sum e^x, and the `top` (0 .. 32) most probable tokens: top_ids int32 [rows][top], top_logp float [rows][top], most probable
    first, equal ones by lowest id.  ids and logp may both be NULL.  Logits of -inf have probability 0; a row of nothing else gives lse =
    logp = top_logp = -inf and entropy 0.  A row with NaN or +inf gives NaN.  work: l2l_op_token_logprobs_work_bytes bytes (may be 0),
-   16-byte aligned, or NULL, which leaves calls of few rows to one workgroup each. */
+   16-byte aligned, or NULL, which leaves calls of few rows to one workgroup each.  At most 2^22 rows a call. */
 int l2l_op_token_logprobs(l2l_ctx*, int dtype, int rows, int vocab, const void* logits, long long ld, const int32_t* ids, float* logp,
                           float* entropy, float* lse, int top, int32_t* top_ids, float* top_logp, void* work);
 /* dlogits ([rows, vocab], row stride ldd, dtype of the logits; in place allowed) from the gradients of logp and of entropy (float [rows],

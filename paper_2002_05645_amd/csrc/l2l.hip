@@ -2344,10 +2344,10 @@ static const char* attention_desc_error(const l2l_attention* a) {
   if (a->head_dim < 8 || a->head_dim > 128 || a->head_dim % 8) return "head_dim must be a multiple of 8 from 8 to 128";
   if (a->sequences < 0 || a->rows < 0 || a->max_len < 0 || a->max_len > 262144) return "sequences, rows and max_len (at most 262144) must not be negative";
   if (!a->first && (long long)a->sequences * a->max_len > a->rows) return "without `first`, sequences x max_len must not exceed rows";
-  if (!(a->scale > 0.f) || !std::isfinite(a->scale)) return "scale must be positive and finite";
+  if (!(a->scale >= 0x1p-64f && a->scale <= 0x1p64f)) return "scale must be positive and finite, from 2^-64 to 2^64";
   if (!drop_threshold(a->dropout, 256, &drop)) return "dropout must be 0, or from 1/512 to 511/512 (it is taken to the nearest 1/256)";
   if (((uintptr_t)a->first | (uintptr_t)a->len) & 3 || (uintptr_t)a->step & 7) return "misaligned first, len or step";
-  if ((long long)a->sequences * a->heads * ((a->max_len + 127) / 128) > (1LL << 22)) return "too many (sequence, head, query block)s for one launch";
+  if ((long long)a->sequences * a->heads * ((a->max_len + 127) / 128) > (1LL << 23)) return "too many (sequence, head, query block)s for one launch";
   return nullptr;
 }
 
@@ -2481,13 +2481,16 @@ int l2l_op_attention_bwd(l2l_ctx* c, const l2l_attention* a, const void* q, long
 
 static bool dropout_rows_ok(int dtype, const void* p, long long ld, int n) { return p && (uintptr_t)p % esize(dtype) == 0 && ld >= n; }
 
-size_t l2l_op_dropout_work_bytes(int rows, int n) { return rows > 0 && n > 0 ? (size_t)dropout_row_blocks(rows, n) * (size_t)n * 4 : 0; }
+constexpr int kMaxBiasColumns = 1 << 25;   // (of the launch that adds the partial sums up)
+
+size_t l2l_op_dropout_work_bytes(int rows, int n) { return rows > 0 && n > 0 && rows <= 1 << 30 && n <= kMaxBiasColumns ? (size_t)dropout_row_blocks(rows, n) * (size_t)n * 4 : 0; }
 
 // what both directions check; drop receives the threshold
 static int dropout_check(l2l_ctx* c, const char* who, int dtype, int rows, int n, const void* x, long long ldx, const void* y, long long ldy, double p,
                          const uint64_t* step, uint32_t* drop) {
   if (!dtype_ok(dtype)) return fail(c, L2L_E_ARG, "%s: bad dtype", who);
   if (rows < 0 || n < 0) return fail(c, L2L_E_ARG, "%s: negative size", who);
+  if (rows > 1 << 30 || n > 1 << 30) return fail(c, L2L_E_ARG, "%s: more than 2^30 rows or columns", who);
   if (!drop_threshold(p, 65536, drop)) return fail(c, L2L_E_ARG, "%s: p must be 0, or from 2^-17 to 1 - 2^-17 (it is taken to the nearest 1/65536)", who);
   if ((uintptr_t)step & 7) return fail(c, L2L_E_ARG, "%s: misaligned step", who);
   if (rows == 0 || n == 0) return L2L_OK;
@@ -2519,6 +2522,7 @@ int l2l_op_dropout_bwd(l2l_ctx* c, int dtype, int rows, int n, const void* dy, l
   memset(&g, 0, sizeof(g));
   L2L_TRY(dropout_check(c, "l2l_op_dropout_bwd", dtype, rows, n, dy, lddy, dx, lddx, p, step, &g.drop));
   if (dbias && ((uintptr_t)dbias & 3 || !work || (uintptr_t)work & 15)) return fail(c, L2L_E_ARG, "l2l_op_dropout_bwd: misaligned dbias, or null or misaligned work");
+  if (dbias && n > kMaxBiasColumns) return fail(c, L2L_E_ARG, "l2l_op_dropout_bwd: dbias of more than 2^25 columns");
   if (n == 0) return L2L_OK;
   if (rows == 0) {   // the sum over no rows
     if (!dbias || accumulate) return L2L_OK;
@@ -2540,7 +2544,8 @@ size_t l2l_op_token_logprobs_work_bytes(int rows, int vocab, int top) {
 static int logprob_check(l2l_ctx* c, const char* who, int dtype, int rows, int vocab, const void* logits, long long ld, const int32_t* ids) {
   if (!dtype_ok(dtype)) return fail(c, L2L_E_ARG, "%s: bad dtype", who);
   if (rows < 0 || vocab <= 0 || vocab > (1 << 30)) return fail(c, L2L_E_ARG, "%s: rows must not be negative, vocab from 1 to 2^30", who);
-  if ((long long)rows * ((vocab + 1023) / 1024 + 32) > (1LL << 31) - 1) return fail(c, L2L_E_ARG, "%s: rows x vocab too large for one launch", who);
+  // (a launch has fewer than 2^32 threads: 512 to a row, 256 to 4096 logits)
+  if (rows > 1 << 22 || (long long)rows * ((vocab + 4095) / 4096) > 1 << 23) return fail(c, L2L_E_ARG, "%s: too many rows for one launch (at most 2^22, and 2^35 logits)", who);
   if (rows == 0) return L2L_OK;
   if (!logits || (uintptr_t)logits % esize(dtype) || ld < vocab) return fail(c, L2L_E_ARG, "%s: null or misaligned logits, or rows shorter than vocab", who);
   if ((uintptr_t)ids & 3) return fail(c, L2L_E_ARG, "%s: misaligned ids", who);

@@ -80,9 +80,9 @@ class Problem:
         ctx.op_attention_bwd(self.plan, self.q, self.q.stride(0), self.k, self.k.stride(0), self.v, self.v.stride(0), self.o, self.o.stride(0), self.lse,
                              self.do, self.do.stride(0), self.dq, self.dq.stride(0), self.dk, self.dk.stride(0), self.dv, self.dv.stride(0), self.work)
 
-    def check(self, seqs=None, heads=None):
+    def check(self, seqs=None, heads=None, scale=None):
         """every entry of o, lse, dq, dk, dv against the oracle, and that nothing else was written"""
-        d, scale, u, low = self.d, self.d ** -0.5, U[self.dtype], LOW[self.dtype]
+        d, scale, u, low = self.d, self.d ** -0.5 if scale is None else scale, U[self.dtype], LOW[self.dtype]
         host = {x: to_host(getattr(self, x)) for x in ("q", "k", "v", "do", "o", "dq", "dk", "dv", "lse")}
         for x in ("o", "dq", "dk", "dv"):
             cols = d * (self.heads if x in ("o", "dq") else self.kv)
@@ -781,3 +781,38 @@ def test_a_fine_tuning_layer_out_of_single_operations(ctx, dtype):
     tol = 12 * U[dtype] if dtype != "fp32" else 2e-6
     for name, got, ref in (("logp", logp, logp_), ("entropy", ent, ent_), ("dlogits", dz, dz_), ("dbias", dbo, dout_.sum(0)), ("dqkv", dqkv, dqkv_), ("dX", dX, dX_)):
         assert O.rel_l2(to_host(got), ref) < tol, (name, O.rel_l2(to_host(got), ref))
+
+
+def test_sizes_that_one_launch_does_not_hold_are_refused(ctx):
+    x = torch.zeros(64, device="cuda")
+    i = torch.zeros(64, dtype=torch.int32, device="cuda")
+    with pytest.raises(P.L2LError, match="2\\^30"):
+        ctx.op_dropout(P.DTYPES["fp32"], 2 ** 30 + 1, 8, x, 8, x, 8, 0.1, 1, 1)
+    with pytest.raises(P.L2LError, match="2\\^30"):
+        ctx.op_dropout(P.DTYPES["bf16"], 1, 2 ** 31 - 9, x, 2 ** 31, x, 2 ** 31, 0.1, 1, 1)
+    with pytest.raises(P.L2LError, match="2\\^25"):
+        ctx.op_dropout_bwd(P.DTYPES["fp32"], 1, 2 ** 25 + 1, x, 2 ** 26, x, 2 ** 26, 0.1, 1, 1, dbias=x, work=x)
+    assert P.dropout_work_bytes(1, 2 ** 25 + 1) == 0 and P.dropout_work_bytes(2 ** 30 + 1, 8) == 0
+    for rows, vocab in ((2 ** 22 + 1, 100), (2 ** 20, 2 ** 16)):
+        with pytest.raises(P.L2LError, match="too many rows"):
+            ctx.op_token_logprobs(P.DTYPES["bf16"], rows, vocab, x, vocab, i, x, x, x)
+        with pytest.raises(P.L2LError, match="too many rows"):
+            ctx.op_token_logprobs_bwd(P.DTYPES["bf16"], rows, vocab, x, vocab, i, x, x, x, None, x, vocab)
+    for scale in (1e-30, 1e30, float("inf"), float("nan"), -1.0, 0.0):
+        plan = P.make_attention(dtype="bf16", heads=1, head_dim=8, sequences=1, max_len=4, scale=scale)
+        assert P.attention_work_bytes(plan) == 0
+    plan = P.make_attention(dtype="bf16", heads=64, head_dim=8, sequences=2 ** 18, max_len=1, rows=2 ** 18)
+    assert P.attention_work_bytes(plan) == 0
+    ctx.sync()
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -60, 2.0 ** -12, 0.7])
+def test_attention_of_any_scale(ctx, scale):
+    for dtype in ("bf16", "fp32"):
+        x = Problem(dtype, 2, 1, 64, [200, 33, 2], True, 0.0, seed=3)
+        x.plan = P.make_attention(dtype=dtype, heads=2, kv_heads=1, head_dim=64, sequences=3, max_len=200, rows=x.rows, first=dev_i32(x.first),
+                                  length=dev_i32(x.lengths), causal=True, scale=scale)
+        x.forward(ctx)
+        x.backward(ctx)
+        ctx.sync()
+        x.check(scale=scale)
