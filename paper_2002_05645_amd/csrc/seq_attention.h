@@ -48,14 +48,25 @@ __device__ __forceinline__ float half_sum(float v) { const Halves h = halves(v);
 //   121.  64 ragged sequences of up to 512, dropped: forward 97 in turn, 87 by one, 88 by two, 95 by eight; dQ 147, 133, 129, 135;
 //   dK and dV 146, 134, 132, 147: with eight or more, XCDs get unequal shares.
 // - 0 with fewer: 7 sequences of 1 to 1999 tokens, 4 key heads of 96: forward 74 in turn, 79 by one and 109 by two.
-struct Place { int unit, block; };   // (sequence, key head) and the workgroup's number among those of the unit
-__device__ __forceinline__ Place place(const SeqAttnArgs& a, int per_unit) {
-  const int id = blockIdx.x, run = a.xcd_run * per_unit;
-  if (a.xcd_run && id < a.sequences * a.kv_heads / (8 * a.xcd_run) * 8 * run) {
-    const int turn = id >> 3, at = turn % run;
-    return Place{((turn / run) * 8 + (id & 7)) * a.xcd_run + at / per_unit, at % per_unit};
+struct Place { int b, hk, head, turn, split; };   // sequence, key head, query head of it, block in the order of `blocks`, split of it
+__device__ __forceinline__ Place place(const SeqAttnArgs& a, int group, int blocks, int splits) {
+  const int per_unit = group * blocks * splits, units = a.sequences * a.kv_heads, run = a.xcd_run * per_unit;
+  const int whole = a.xcd_run ? units / (8 * a.xcd_run) * 8 * a.xcd_run : 0;   // units that go to XCDs in runs
+  int id = blockIdx.x, unit, head, turn;
+  const int split = id % splits;
+  if (id < whole * per_unit) {
+    const int round = id >> 3, at = round % run, block = at % per_unit / splits;
+    unit = ((round / run) * 8 + (id & 7)) * a.xcd_run + at / per_unit;
+    head = block / blocks;
+    turn = block % blocks;
+    return Place{unit / a.kv_heads, unit % a.kv_heads, head, turn, at % splits};
   }
-  return Place{id / per_unit, id % per_unit};
+  id = (id - whole * per_unit) / splits;
+  const int rows = (units - whole) * group, of = id % rows;
+  turn = id / rows;
+  unit = whole + of / group;
+  head = of % group;
+  return Place{unit / a.kv_heads, unit % a.kv_heads, head, turn, split};
 }
 
 struct Seq { long long first; int n; };
@@ -167,10 +178,9 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
   __shared__ __attribute__((aligned(1024))) char lds[4 * I::IMG];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, group * nblk * a.splits_fwd);
-  const int split = at.block % a.splits_fwd, of_head = at.block / a.splits_fwd;
-  const int blk = nblk - 1 - of_head % nblk;   // (a causal sequence's longest blocks first)
-  const int b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads, h = hk * group + of_head / nblk, bh = b * a.heads + h;
+  const Place at = place(a, group, nblk, a.splits_fwd);
+  const int split = at.split, blk = nblk - 1 - at.turn;   // (a causal sequence's longest blocks first)
+  const int b = at.b, hk = at.hk, h = hk * group + at.head, bh = b * a.heads + h;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_q = blk * 128;
   if (base_q >= n) return;
@@ -283,10 +293,9 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
   __shared__ __attribute__((aligned(1024))) char lds[4 * I::IMG];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, group * nblk * a.splits_dq);
-  const int split = at.block % a.splits_dq, of_head = at.block / a.splits_dq;
-  const int blk = nblk - 1 - of_head % nblk;
-  const int b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads, h = hk * group + of_head / nblk, bh = b * a.heads + h;
+  const Place at = place(a, group, nblk, a.splits_dq);
+  const int split = at.split, blk = nblk - 1 - at.turn;   // (a causal sequence's longest blocks first)
+  const int b = at.b, hk = at.hk, h = hk * group + at.head, bh = b * a.heads + h;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_q = blk * 128;
   if (base_q >= n) return;
@@ -426,8 +435,8 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   constexpr int KIMG = 2 * STAGE, SIMG = KIMG + 2 * I::IMG, STAT = SIMG + 2 * IS::IMG;   // (WHOLE) K, dS, two heads' -lse and D of 128 rows
   __shared__ __attribute__((aligned(1024))) char lds[WHOLE ? STAT + 2 * 1024 : 2 * STAGE];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, nblk * a.splits_dkv);
-  const int split = at.block % a.splits_dkv, blk = at.block / a.splits_dkv, b = at.unit / a.kv_heads, hk = at.unit % a.kv_heads;
+  const Place at = place(a, 1, nblk, a.splits_dkv);
+  const int split = at.split, blk = at.turn, b = at.b, hk = at.hk;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_k = blk * 128;
   if (base_k >= n) return;
