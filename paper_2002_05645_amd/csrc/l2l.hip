@@ -2414,8 +2414,7 @@ static SeqAttnArgs attention_args(l2l_ctx* c, const l2l_attention* a, const void
   (void)drop_threshold(a->dropout, 256, &g.drop);
   g.seed = a->seed; g.site = a->site; g.step = a->step;
   g.splits_fwd = g.splits_dq = g.splits_dkv = 1;
-  if (2LL * a->max_len * a->head_dim * (long long)esize(a->dtype) >= 2 << 20) g.xcd_run = 1;   // (half of an XCD's L2)
-  else if ((long long)a->sequences * a->kv_heads >= 256) g.xcd_run = a->max_len <= 128 ? 8 : 2;
+  g.by_group = 2 * a->rows * a->kv_heads * a->head_dim * (long long)esize(a->dtype) >= 8 << 20;   // (keys and values against two XCDs' L2)
   g.bad = c->bad_ids;
   return g;
 }

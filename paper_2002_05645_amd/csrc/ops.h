@@ -24,7 +24,7 @@ struct SeqAttnArgs {
   int splits_fwd, splits_dq, splits_dkv;
   float* part;                        // [split][rows][heads d]; dK / dV: [split][2][rows][kv_heads d], dV first
   float* part_lse;                    // forward: [split][heads][rows]
-  int xcd_run;                        // whole (sequence, key head) units that an XCD takes one after the other (0: blocks in turn)
+  int by_group;                       // 1: an XCD takes the query heads that share a key head one after the other
   int32_t* bad;                       // bit 1: a sequence did not fit rows or max_len
 };
 

@@ -38,35 +38,24 @@ __device__ __forceinline__ Halves halves(float v) {
 __device__ __forceinline__ float half_max(float v) { const Halves h = halves(v); return fmaxf(h.lo, h.hi); }
 __device__ __forceinline__ float half_sum(float v) { const Halves h = halves(v); return h.lo + h.hi; }
 
-// Workgroup order.  Consecutive workgroups go to the 8 XCDs in turn, which spreads long and short sequences over the chip: with xcd_run
-// 0 the order is (sequence, key head, query head of it, block) as it stands.  Otherwise an XCD takes xcd_run whole (sequence, key
-// head) units one after the other, as far as runs of them come in eights:
-// - 1 where a head's keys and values are the larger part of an L2: the blocks that read the same ones meet there.  One causal sequence of
-//   16384 tokens, 8 key heads of 128: forward 2650 us in turn, 2200 so, dQ 4540 and 3400, dK and dV 6500 and 4600.
-// - 8 or, with several blocks to a unit, 2 where there are many units (256): heads that lie side by side in memory are read by one XCD
-//   at a time.  256 sequences of 128, 16 heads of 64: forward 70 and 59, backward 154 and 148; ragged, dropped 44.7 and 43.8, 124.5 and
-//   121.  64 ragged sequences of up to 512, dropped: forward 97 in turn, 87 by one, 88 by two, 95 by eight; dQ 147, 133, 129, 135;
-//   dK and dV 146, 134, 132, 147: with eight or more, XCDs get unequal shares.
-// - 0 with fewer: 7 sequences of 1 to 1999 tokens, 4 key heads of 96: forward 74 in turn, 79 by one and 109 by two.
-struct Place { int b, hk, head, turn, split; };   // sequence, key head, query head of it, block in the order of `blocks`, split of it
-__device__ __forceinline__ Place place(const SeqAttnArgs& a, int group, int blocks, int splits) {
-  const int per_unit = group * blocks * splits, units = a.sequences * a.kv_heads, run = a.xcd_run * per_unit;
-  const int whole = a.xcd_run ? units / (8 * a.xcd_run) * 8 * a.xcd_run : 0;   // units that go to XCDs in runs
-  int id = blockIdx.x, unit, head, turn;
-  const int split = id % splits;
-  if (id < whole * per_unit) {
-    const int round = id >> 3, at = round % run, block = at % per_unit / splits;
-    unit = ((round / run) * 8 + (id & 7)) * a.xcd_run + at / per_unit;
-    head = block / blocks;
-    turn = block % blocks;
-    return Place{unit / a.kv_heads, unit % a.kv_heads, head, turn, at % splits};
-  }
-  id = (id - whole * per_unit) / splits;
-  const int rows = (units - whole) * group, of = id % rows;
-  turn = id / rows;
-  unit = whole + of / group;
-  head = of % group;
-  return Place{unit / a.kv_heads, unit % a.kv_heads, head, turn, split};
+// Workgroup order.  Blocks in the order of the launch's `blocks` (the longest walks first, where the mask makes them differ), and of one block
+// all heads of all sequences: long and short sequences then spread over the chip, the longest walks begin first, and the blocks that
+// a short sequence does not have end at once.  (Head by head, the 8 XCDs that take workgroups in turn each get the same blocks of every
+// head, some the long and some the short ones: one causal sequence of 4096, 32 heads on 8 of 64: forward 144 us, 99 so; dQ 180 and 117.
+// 64 ragged sequences of up to 512, 16 heads, dropped: 88 and 80, 112 and 100, dK and dV 134 and 122.)
+// Of these heads an XCD takes runs of neighbours, as far as they come in eights:
+// - the query heads that share a key head, whose keys and values then meet in its L2, where all of them are more than two L2s.  7 causal
+//   sequences of up to 1999, 12 heads on 4 of 96: forward 79 us one by one and 62 in threes, dQ 78 and 66; 6 of up to 1700, 32 heads on 8 of 128:
+//   143 and 139, 185 and 180; but 12 of up to 1200, 16 heads on 2 of 64, 4 MB: 44 and 49, 50 and 59.
+// - eight, where sequences have one block: heads side by side in memory are read by one XCD at a time.  256 of 128 tokens, 16 heads of
+//   64: forward 74 and 61, backward 155 and 149.  (With 64 of 512: 80 and 85, 100 and 106: XCDs get unequal shares of ragged sequences.)
+struct Place { int b, hk, head, turn, split; };   // sequence, key head, query head of it, block in order, split of it
+__device__ __forceinline__ Place place(const SeqAttnArgs& a, int group, int splits) {
+  const int run = a.max_len <= 128 ? 8 : a.by_group ? group : 1, of_turn = a.sequences * a.kv_heads * group * splits;
+  const int turn = blockIdx.x / of_turn, in = blockIdx.x % of_turn;
+  const int at = in < of_turn / (8 * run) * (8 * run) ? in / (8 * run) * (8 * run) + (in & 7) * run + (in >> 3) % run : in;
+  const int head = at / splits, unit = head / group;
+  return Place{unit / a.kv_heads, unit % a.kv_heads, head % group, turn, at % splits};
 }
 
 struct Seq { long long first; int n; };
@@ -178,7 +167,7 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
   __shared__ __attribute__((aligned(1024))) char lds[4 * I::IMG];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, group, nblk, a.splits_fwd);
+  const Place at = place(a, group, a.splits_fwd);
   const int split = at.split, blk = nblk - 1 - at.turn;   // (a causal sequence's longest blocks first)
   const int b = at.b, hk = at.hk, h = hk * group + at.head, bh = b * a.heads + h;
   const Seq sq = sequence(a, b);
@@ -293,7 +282,7 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
   __shared__ __attribute__((aligned(1024))) char lds[4 * I::IMG];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, group, nblk, a.splits_dq);
+  const Place at = place(a, group, a.splits_dq);
   const int split = at.split, blk = nblk - 1 - at.turn;   // (a causal sequence's longest blocks first)
   const int b = at.b, hk = at.hk, h = hk * group + at.head, bh = b * a.heads + h;
   const Seq sq = sequence(a, b);
@@ -435,7 +424,7 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   constexpr int KIMG = 2 * STAGE, SIMG = KIMG + 2 * I::IMG, STAT = SIMG + 2 * IS::IMG;   // (WHOLE) K, dS, two heads' -lse and D of 128 rows
   __shared__ __attribute__((aligned(1024))) char lds[WHOLE ? STAT + 2 * 1024 : 2 * STAGE];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, 1, nblk, a.splits_dkv);
+  const Place at = place(a, 1, a.splits_dkv);
   const int split = at.split, blk = at.turn, b = at.b, hk = at.hk;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_k = blk * 128;

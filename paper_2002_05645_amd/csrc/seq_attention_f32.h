@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256) void seq_fwd_f32_kernel(const SeqAttnArgs a) {
   using I = ImgF<DP>;
   __shared__ __attribute__((aligned(16))) float lds[PARTS * 2 * I::FLOATS];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, group, nblk, a.splits_fwd);
+  const Place at = place(a, group, a.splits_fwd);
   const int split = at.split, blk = nblk - 1 - at.turn, b = at.b, hk = at.hk, h = hk * group + at.head, bh = b * a.heads + h;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_q = blk * 128;
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(256) void seq_bwd_dq_f32_kernel(const SeqAttnArgs a
   using I = ImgF<DP>;
   __shared__ __attribute__((aligned(16))) float lds[PARTS * 2 * I::FLOATS];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, group, nblk, a.splits_dq);
+  const Place at = place(a, group, a.splits_dq);
   const int split = at.split, blk = nblk - 1 - at.turn, b = at.b, hk = at.hk, h = hk * group + at.head, bh = b * a.heads + h;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_q = blk * 128;
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(256) void seq_bwd_dkv_f32_kernel(const SeqAttnArgs 
   constexpr int STAGE = 2 * I::FLOATS + 64;   // Q, dO, and 32 rows' lse and D
   __shared__ __attribute__((aligned(16))) float lds[PARTS * STAGE];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
-  const Place at = place(a, 1, nblk, a.splits_dkv);
+  const Place at = place(a, 1, a.splits_dkv);
   const int split = at.split, blk = at.turn, b = at.b, hk = at.hk;
   const Seq sq = sequence(a, b);
   const int n = sq.n, base_k = blk * 128;
