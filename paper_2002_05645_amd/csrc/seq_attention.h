@@ -159,7 +159,7 @@ __device__ __forceinline__ void store_part(const f32x16 (&acc)[DP / 32], float* 
 // look at the rows' maxima and saves 16 registers: a fourth wave a SIMD at 64 columns also with dropped probabilities.
 // Bound at 64 columns by vector instructions (109 of them, 16 exponentials, to 8 MFMA per wave and 32 keys; 62 % of the SIMDs' clocks at
 // three or more waves), at 128 by the matrix cores.  256 sequences of 128 tokens, 16 heads of 64: 60 us, 4.5 TB/s of the 5.1 that a copy
-// reaches; 64 of 512: 102 to 116 us.  One causal sequence of 16384, 32 heads on 8 of 128: 2200 to 2300 us, 970 TFLOP/s of the visible half
+// reaches; 64 of up to 512, ragged and dropped: 80 us.  One causal sequence of 16384, 32 heads on 8 of 128: 2200 to 2300 us, 970 TFLOP/s of the visible half
 // (a library product of 8192^3: 1221).
 template <typename E, int DP, bool DROP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 64 ? 4 : DP <= 96 && DROP ? 3 : 2)))
@@ -274,8 +274,7 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
 
 // ---- dQ, and what the dK / dV kernel needs of each row ----------------------------------------------------------------
 // As the forward kernel, with dP beside S and dS K in the place of P V.  Bound by vector instructions and the latency of its three dependent
-// products at 64 columns (64 of 512 tokens, 16 heads: 163 us, 630 TFLOP/s; 124 us at two waves a SIMD and 114 at three with dropped
-// probabilities and ragged lengths), by the matrix cores at 128 (one causal sequence of 16384, 32 heads on 8: 2950 us, 1120 TFLOP/s).
+// products at 64 columns (64 sequences of up to 512, 16 heads, dropped: 98 us; at two waves a SIMD a tenth more), by the matrix cores at 128 (one causal sequence of 16384, 32 heads on 8: 2950 us, 1120 TFLOP/s).
 template <typename E, int DP, bool DROP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 32 ? 4 : DP <= 64 ? 3 : 2)))
 void seq_bwd_dq_kernel(const SeqAttnArgs a) {
@@ -413,7 +412,7 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
 // rows' D and lse are taken from O, dO and lse at the head's start.  (256 sequences of up to 128, 16 heads of 64, dropped: 119 us, the two
 // kernels 143; wider heads leave no registers for it.)
 // Bound at 64 columns by latency at two waves a SIMD (235 to 256 registers; at three they spill): 64 ragged sequences of up to 512, dropped,
-// 130 us; WHOLE by its first loads, half of a workgroup's life (256 of 128 tokens: 143 us, 3.7 TB/s), at 128 columns, one wave a SIMD,
+// 121 us; WHOLE by its first loads, half of a workgroup's life (256 of 128 tokens: 143 us, 3.7 TB/s), at 128 columns, one wave a SIMD,
 // by the matrix cores (one causal sequence of 16384, 32 heads on 8: 4600 us, 955 TFLOP/s).
 template <typename E, int DP, bool DROP, bool WHOLE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP > 96 ? 1 : 2)))
