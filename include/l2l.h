@@ -377,7 +377,7 @@ int l2l_op_attention(l2l_ctx*, const l2l_attention*, const void* q, long long ld
 int l2l_op_attention_bwd(l2l_ctx*, const l2l_attention*, const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv,
                          const void* o, long long ldo, const float* lse, const void* dout, long long lddo, void* dq, long long lddq,
                          void* dk, long long lddk, void* dv, long long lddv, void* work);
-/* 0 on a bad description. */
+/* From dtype, heads, kv_heads, head_dim, sequences, max_len and rows alone; 0 on a bad description. */
 size_t l2l_op_attention_work_bytes(const l2l_attention*);
 
 /* y = resid + drop(x + bias), [rows, n] with row strides in elements of any alignment; bias [n] and resid may be NULL; in

@@ -2393,8 +2393,15 @@ static AttentionSplits attention_plan(const l2l_attention* a) {
 
 size_t l2l_op_attention_work_bytes(const l2l_attention* a) {
   if (attention_desc_error(a)) return 0;
-  const AttentionSplits p = attention_plan(a);
-  return std::max(p.fwd_bytes, p.bwd_bytes);
+  size_t most = 0;   // (the same for training and evaluation, masked or not: one buffer does for all)
+  for (int i = 0; i < 4; ++i) {
+    l2l_attention like = *a;
+    like.causal = i & 1;
+    like.dropout = i & 2 ? 0.5 : 0.0;
+    const AttentionSplits p = attention_plan(&like);
+    most = std::max(most, std::max(p.fwd_bytes, p.bwd_bytes));
+  }
+  return most;
 }
 
 // rows of `heads` heads as the kernels read and write them

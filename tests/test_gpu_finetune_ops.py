@@ -694,6 +694,47 @@ def test_captured_calls_replay_and_take_a_new_mask_with_the_step():
         c.close()
 
 
+def test_captured_calls_in_parts_share_one_workspace():
+    # two captured graphs (a training and an evaluation pass) over sequences long enough for parts, one workspace, replayed in turn
+    stream = torch.cuda.Stream()
+    c = P.Context(P.make_config(64, 2, 128, 16, 2, 2, "bf16", 1e-5, 0), stream.cuda_stream, stream.cuda_stream)
+    try:
+        for dtype in ("bf16", "fp32"):
+            x = Problem(dtype, 4, 1, 64, [900, 70], True, 0.2, seed=31)
+            calm = P.make_attention(dtype=dtype, heads=4, kv_heads=1, head_dim=64, sequences=2, max_len=900, rows=x.rows, first=dev_i32(x.first), length=dev_i32(x.lengths))
+            assert P.attention_work_bytes(calm) == P.attention_work_bytes(x.plan) > 4 * x.rows * 8
+            train = x.plan
+
+            def body():
+                x.forward(c)
+                x.backward(c)
+            graphs, eager = [], []
+            for plan, what in ((train, body), (calm, lambda: x.forward(c))):
+                x.plan = plan
+                torch.cuda.synchronize()
+                what()
+                torch.cuda.synchronize()
+                eager.append([t.clone() for t in (x.o, x.lse, x.dq, x.dk, x.dv)])
+                graphs.append(_captured(stream, what))
+            for which in (0, 1, 0, 0, 1, 0):
+                for t in (x.o, x.lse) if which else (x.o, x.lse, x.dq, x.dk, x.dv):
+                    t.fill_(7.0)
+                x.work.fill_(255)
+                torch.cuda.synchronize()
+                with torch.cuda.stream(stream):
+                    graphs[which].replay()
+                torch.cuda.synchronize()
+                torch.randn(1000, device="cuda").sum().item()
+                assert all(torch.equal(a, b) for a, b in zip((x.o, x.lse, x.dq, x.dk, x.dv)[:2 if which else 5], eager[which]))
+            x.plan = train
+            with torch.cuda.stream(stream):
+                graphs[0].replay()
+            torch.cuda.synchronize()
+            x.check()
+    finally:
+        c.close()
+
+
 def test_two_contexts_on_two_streams_at_once():
     streams = [torch.cuda.Stream() for _ in range(2)]
     cs = [P.Context(P.make_config(64, 2, 128, 16, 2, 2, "bf16", 1e-5, 0), s.cuda_stream, s.cuda_stream) for s in streams]
