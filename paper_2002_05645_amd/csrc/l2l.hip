@@ -2370,7 +2370,23 @@ static int attention_splits(double wgs, int tiles, double total, double us_per_t
   return best_s;
 }
 
+// The same for the backward kernel that has all keys of a head: parts of whole query heads.  A head's tile takes 4 us (two workgroups on a
+// compute unit).  128 ragged sequences of up to 128, 16 heads on 2 of 64, dropped: 83 us, in two parts 59 + 8; 40 of up to 100, 12 heads on 4: 34,
+// 20 + 6; 128 of 128, 16 heads on 4, whose 512 workgroups fill the chip, stay whole at 52.
+static int attention_head_splits(double wgs, int group, int tiles, double bytes) {
+  int best_s = 1;
+  double best = 1e300;
+  for (int s = 1; s <= group && (s == 1 || wgs * s <= 512); ++s) {
+    if (group % s) continue;
+    const double us = group / s * tiles * 4.0 + (s > 1 ? 4.0 + s * bytes / 5.0e6 : 0.0);
+    if (us < best * 0.9) { best = us; best_s = s; }
+  }
+  return best_s;
+}
+
 struct AttentionSplits { int fwd, dq, dkv; size_t fwd_bytes, bwd_bytes; };   // bytes of workspace of either call
+// the backward pass in one kernel: a workgroup has all of a head's keys (wider heads leave no registers for it)
+static bool attention_in_one(const l2l_attention* a) { return is16(a->dtype) && a->max_len <= 128 && a->head_dim <= 64; }
 static AttentionSplits attention_plan(const l2l_attention* a) {
   AttentionSplits p = {1, 1, 1, 0, 0};
   const double rows = (double)a->rows, q = rows * a->heads, kv = rows * a->kv_heads;
@@ -2384,7 +2400,8 @@ static AttentionSplits attention_plan(const l2l_attention* a) {
     // of a tile (16-bit formats: 1.1 us at 64 columns, 2.1 at 128, 1.8 and 2.4 at 64 and 96 dropped; fp32: 3.4 to 7.2 at 64)
     const double us = is16(a->dtype) ? std::max(0.8, a->head_dim / 60.0) + (a->dropout > 0 ? 0.7 : 0.0) : std::max(2.0, a->head_dim / 13.0);
     p.fwd = p.dq = attention_splits(blocks * a->heads, tiles, total, us, q * a->head_dim * 4);
-    p.dkv = attention_splits(blocks * a->kv_heads, tiles * group, total, us, 2 * kv * a->head_dim * 4);
+    if (attention_in_one(a)) p.dkv = attention_head_splits((double)a->sequences * a->kv_heads, group, tiles, 2 * kv * a->head_dim * 4);
+    else p.dkv = attention_splits(blocks * a->kv_heads, tiles * group, total, us, 2 * kv * a->head_dim * 4);
   }
   if (p.fwd > 1) p.fwd_bytes = (size_t)(p.fwd * q * (a->head_dim + 1)) * 4;
   p.bwd_bytes = stats + (size_t)std::max(p.dq > 1 ? p.dq * q * a->head_dim * 4 : 0.0, p.dkv > 1 ? p.dkv * 2 * kv * a->head_dim * 4 : 0.0);
@@ -2478,7 +2495,7 @@ int l2l_op_attention_bwd(l2l_ctx* c, const l2l_attention* a, const void* q, long
   g.o = o; g.ldo = ldo; g.lse = (float*)lse; g.dout = dout; g.lddo = lddo;
   g.dq = dq; g.lddq = lddq; g.dk = dk; g.lddk = lddk; g.dv = dv; g.lddv = lddv;
   const AttentionSplits p = attention_plan(a);
-  g.splits_dq = p.dq; g.splits_dkv = p.dkv;
+  g.in_one = attention_in_one(a); g.splits_dq = p.dq; g.splits_dkv = p.dkv;
   g.nlse2 = (float*)work;
   g.delta = g.nlse2 + (long long)a->heads * a->rows;
   g.part = g.nlse2 + (2 * (long long)a->heads * a->rows + 3) / 4 * 4;

@@ -22,6 +22,7 @@ struct SeqAttnArgs {
   // Splits over the long axis: of a query block's keys (forward, dQ) and of a key block's queries and query
   // heads (dK / dV).  Above 1 the kernels leave fp32 partial results that a second kernel adds up.
   int splits_fwd, splits_dq, splits_dkv;
+  int in_one;                         // backward: one kernel for all three gradients; splits_dkv then divides the query heads of a key head
   float* part;                        // [split][rows][heads d]; dK / dV: [split][2][rows][kv_heads d], dV first
   float* part_lse;                    // forward: [split][heads][rows]
   int by_group;                       // 1: an XCD takes the query heads that share a key head one after the other

@@ -83,9 +83,10 @@ void L2L_NAME(l2l_seq_attn_bwd_)(const SeqAttnArgs& a, hipStream_t s) {
 #else
   const auto both = [&](auto drop) {
     constexpr bool D = decltype(drop)::value;
-    if constexpr (L2L_DP <= 64) {   // (wider heads leave no registers for it)
-      if (a.max_len <= 128 && a.splits_dkv == 1) {       // a workgroup has all of a head's keys: one kernel does both
-        go(sattn::seq_bwd_dkv_kernel<Elem, L2L_DP, D, true>, blocks(a, a.kv_heads, 128), a, s);
+    if constexpr (L2L_DP <= 64) {
+      if (a.in_one) {
+        go(sattn::seq_bwd_dkv_kernel<Elem, L2L_DP, D, true>, blocks(a, a.kv_heads * a.splits_dkv, 128), a, s);
+        join_dkv(a, s);
         return;
       }
     }
