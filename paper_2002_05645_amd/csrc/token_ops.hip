@@ -217,6 +217,7 @@ void launch_dropout_t(const DropoutArgs& a, hipStream_t s) {
 // Bound by memory: two workgroups of 512 threads share a compute unit and load under each other's reductions.
 // Rows too few to fill the chip are split over workgroups, whose parts a second kernel joins.
 constexpr int LP_LIST = 1024, LP_TOP = 32;
+constexpr float LP_NEAR = 0x1p20f;   // (half a step of x log2(e) is 1/16 at most below it)
 constexpr float LP_FAR = -1.0e4f;   // 2^x is 0 from here down, and 0 * x has to be 0 as well for x = -inf
 constexpr float LP_LOG2E = 1.4426950408889634f, LP_LN2 = 0.6931471805599453f;
 
@@ -229,15 +230,17 @@ __device__ __forceinline__ float key_value(uint32_t k) { return __builtin_bit_ca
 // larger = earlier in the top: the value, then the lower index
 __device__ __forceinline__ uint64_t rank_key(uint32_t key, uint32_t index) { return (uint64_t)key << 32 | (0xFFFFFFFFu - index); }
 
-// In powers of two: m = the largest x log2(e), s = sum 2^(x log2(e) - m), t = sum 2^(..) (x log2(e) - m).  (m may be rounded: every
-// exponent is taken against the same rounded one, in one fma.)
+// m = the largest x, s = sum 2^d, t = sum 2^d d with d = (x - m) log2(e).  m is a logit itself and every difference is taken before its
+// product: a rounded m log2(e) is off by half a step of its own, which is a factor of the sums wherever logits are far from zero (a
+// vocabulary masked with -1e10 or the type's lowest value: 2^128 and more), and overflows from 2.4e38 on.
 struct Stat { float m, s, t; };
+__device__ __forceinline__ float log2_ratio(float x, float m) { return fmaxf((x - m) * LP_LOG2E, LP_FAR); }   // (NaN becomes LP_FAR)
 // both relative to their own maximum; an empty one (m = -inf, s = t = 0) changes nothing
 __device__ __forceinline__ Stat join(Stat a, Stat b) {
   Stat r;
   r.m = fmaxf(a.m, b.m);
   if (r.m == -INFINITY) return Stat{r.m, a.s + b.s, a.t + b.t};
-  const float da = fmaxf(a.m - r.m, LP_FAR), db = fmaxf(b.m - r.m, LP_FAR), fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+  const float da = log2_ratio(a.m, r.m), db = log2_ratio(b.m, r.m), fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
   r.s = a.s * fa + b.s * fb;
   r.t = (a.t + a.s * da) * fa + (b.t + b.s * db) * fb;
   return r;
@@ -245,7 +248,7 @@ __device__ __forceinline__ Stat join(Stat a, Stat b) {
 __device__ __forceinline__ Stat wave_join(Stat a) {
   Stat r;
   r.m = wave_max(a.m);
-  const float d = r.m == -INFINITY ? 0.f : fmaxf(a.m - r.m, LP_FAR), f = __builtin_amdgcn_exp2f(d);
+  const float d = r.m == -INFINITY ? 0.f : log2_ratio(a.m, r.m), f = __builtin_amdgcn_exp2f(d);
   r.s = wave_sum(a.s * f);
   r.t = wave_sum((a.t + a.s * d) * f);
   return r;
@@ -272,12 +275,12 @@ __device__ __forceinline__ uint32_t lanes_reach(uint32_t key, int count) {
 
 // log p of a logit x of the row
 __device__ __forceinline__ float log_prob(Stat st, float x) {
-  return st.m == -INFINITY ? -INFINITY : (fmaf(x, LP_LOG2E, -st.m) - log2f(st.s)) * LP_LN2;
+  return st.m == -INFINITY ? -INFINITY : (x - st.m) - log2f(st.s) * LP_LN2;
 }
 __device__ __forceinline__ void write_row(const LogprobArgs& a, int row, Stat st, int id, float x_id) {
   const bool none = st.m == -INFINITY;   // every logit is -inf
   const float log_s = log2f(st.s);
-  a.lse[row] = none ? -INFINITY : (st.m + log_s) * LP_LN2;
+  a.lse[row] = none ? -INFINITY : fmaf(log_s, LP_LN2, st.m);
   a.entropy[row] = none ? 0.f : (log_s - st.t / st.s) * LP_LN2;
   if (id >= a.vocab) atomicOr(a.bad, 1);   // (clamped)
   if (a.ids) a.logp[row] = id < 0 ? 0.f : log_prob(st, x_id);
@@ -357,16 +360,35 @@ void logprob_kernel(const LogprobArgs a) {
         }
       };
       forget();
-      Stat mine = {lm == -INFINITY ? lm : lm * LP_LOG2E, 0.f, 0.f};
-      const float base = lm == -INFINITY ? 0.f : mine.m;
+      // One fma a value, x log2(e) - lm log2(e) with the second product rounded, and what that rounding left out (up to 1/16) taken out of the
+      // sums behind; where a maximum of the wave lies too far from zero for it, the difference first.  (4915 rows of 30522 in fp32: 117 us; the
+      // difference first everywhere 120; 16-bit rows take as long either way.)
+      Stat mine = {lm, 0.f, 0.f};
+      const float own_m = lm == -INFINITY ? 0.f : lm;
+      const auto add = [&](float d) {
+        const float e = __builtin_amdgcn_exp2f(d);
+        mine.s += e;
+        mine.t = fmaf(e, fmaxf(d, LP_FAR), mine.t);
+      };
+      if (__any(!(fabsf(own_m) < LP_NEAR))) {
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
+        for (int j = 0; j < NV; ++j) {
+          u32x4 raw = __builtin_bit_cast(u32x4, r[j]);   // (a copy that shares nothing with the other branch)
+          asm("" : "+v"(raw));
+          const Line16 line = __builtin_bit_cast(Line16, raw);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float d = fmaf(to_f32(r[j].v[i]), LP_LOG2E, -base), e = __builtin_amdgcn_exp2f(d);
-          mine.s += e;
-          mine.t = fmaf(e, fmaxf(d, LP_FAR), mine.t);
+          for (int i = 0; i < N; ++i) add((to_f32(line.v[i]) - own_m) * LP_LOG2E);
         }
+      } else {
+        const float base = own_m * LP_LOG2E, rest = fmaf(own_m, LP_LOG2E, -base);   // own_m log2(e) = base + rest
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+          for (int i = 0; i < N; ++i) add(fmaf(to_f32(r[j].v[i]), LP_LOG2E, -base));
+        const float back = __builtin_amdgcn_exp2f(-rest);
+        mine.t = (mine.t - mine.s * rest) * back;
+        mine.s *= back;
+      }
       st = join(st, wave_join(mine));
       if (top) {
         // The bound may be any that is one: if each of t waves has q lanes whose maxima reach b, and t q >= top, then b is.  The first

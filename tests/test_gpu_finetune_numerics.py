@@ -1,0 +1,88 @@
+"""GPU tests of the single fine-tuning operations at the ends of their numbers: masked and far-away logits, NaN, scores of any size, small
+gradients, and what l2l_sync reports.
+
+Expected values are computed in fp64 relative to each row's maximum, where a fill of the type's lowest value leaves nothing to cancel."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2002_05645_amd as P
+from oracle import finetune_oracle as F
+from gpu_util import to_host
+from test_gpu_finetune_ops import E24, LOW, SEED, SITE, TDT, U, Problem, _logprobs, ctx, dev_i32  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------- token log probabilities
+def _row_reference(x, ids, top):
+    """logp, entropy, lse, top ids, their log probabilities, log p of every token; x: rows of fp64 without NaN or +inf"""
+    with np.errstate(invalid="ignore", divide="ignore"):
+        m = x.max(-1, keepdims=True)
+        d = np.where(np.isneginf(x), -np.inf, x - m)
+        e = np.exp(d)
+        s = e.sum(-1, keepdims=True)
+        lp = d - np.log(s)
+        entropy = np.log(s) - np.where(e > 0, e * np.where(e > 0, d, 0.0), 0.0).sum(-1, keepdims=True) / s
+        lse = m + np.log(s)
+    order = np.stack([np.lexsort((np.arange(x.shape[1]), -row)) for row in x])[:, :top]
+    logp = np.where(ids >= 0, lp[np.arange(len(ids)), np.maximum(ids, 0)], 0.0)
+    return logp, entropy[:, 0], lse[:, 0], order, np.take_along_axis(lp, order, 1), lp
+
+
+def _check_rows(r, ids, top, dtype):
+    x, ids = r["x"], np.asarray(ids)
+    logp, entropy, lse, order, top_logp, _ = _row_reference(x, ids, top)
+    # differences to the maximum that an exponential can tell from minus infinity
+    near = np.minimum(np.where(np.isfinite(x), x.max(-1, keepdims=True) - x, 0.0), 104.0).max(-1)
+    # sums of at most 64 terms a thread and a dozen joins, exponentials whose argument is off by `near` roundings, logarithms
+    f = (96 + 4 * near) * E24
+    same = lambda a, b, tol: ((np.abs(a - b) <= tol) | (a == b)).all()  # noqa: E731
+    assert same(to_host(r["lse"]), lse, f + 2 * E24 * np.abs(lse))
+    assert same(to_host(r["logp"]), logp, f + 4 * E24 * np.abs(logp))
+    assert same(to_host(r["entropy"]), entropy, 2 * f * (1 + near))
+    assert np.array_equal(r["top_ids"].cpu().numpy(), order)
+    assert same(to_host(r["top_logp"]), top_logp, f[:, None] + 4 * E24 * np.abs(top_logp))
+
+
+def _masked_rows(dtype, fill, rows, vocab):
+    """rows masked with `fill` in the ways that programs mask: all but two tokens, everything, a block in front, every second token, together with -inf"""
+    rng = np.random.default_rng(vocab + rows)
+    x = (rng.normal(size=(rows, vocab)) * 3).astype(np.float32)
+    fill = torch.finfo(TDT[dtype]).min if fill == "lowest" else fill
+    keep = x[0, [vocab // 3, vocab - 1]]
+    x[0] = fill
+    x[0, [vocab // 3, vocab - 1]] = keep
+    x[1] = fill
+    x[2, :vocab // 2] = fill
+    x[3, ::2] = fill
+    x[4, : vocab - 2] = fill
+    x[4, : vocab // 4] = -np.inf
+    ids = rng.integers(0, vocab, rows)
+    ids[:5] = [vocab - 1, 7, 3, 1, vocab - 3]     # of allowed tokens and of masked ones
+    return x, ids
+
+
+MASKED = [(5, 300), (600, 1000), (5, 9000), (5, 40001), (300, 40001), (5, 140000)]   # one slab, several, several rows a workgroup, split rows
+
+
+@pytest.mark.parametrize("rows,vocab", MASKED)
+@pytest.mark.parametrize("dtype,fill", [("fp32", -1e10), ("fp32", -1e30), ("fp32", "lowest"), ("bf16", -1e10), ("bf16", -1e30), ("bf16", "lowest"), ("fp16", "lowest"), ("fp32", -1e9), ("bf16", -1e4)])
+def test_logprobs_of_masked_vocabularies(ctx, dtype, fill, rows, vocab):  # noqa: F811
+    x, ids = _masked_rows(dtype, fill, rows, vocab)
+    for work in (True, False):
+        r = _logprobs(ctx, dtype, x, ids, 6, vocab + 3, work)
+        ctx.sync()
+        _check_rows(r, ids, 6, dtype)
+
+
+@pytest.mark.parametrize("dtype,offset", [("fp32", 300.0), ("fp32", -1.0e4), ("fp32", 2.0e6), ("bf16", 1.0e3), ("fp16", 2.0e4)])
+@pytest.mark.parametrize("rows,vocab", [(4, 2000), (3, 40001), (3, 140000)])
+def test_logprobs_do_not_depend_on_a_common_offset(ctx, dtype, offset, rows, vocab):  # noqa: F811
+    # log p and the entropy are functions of the differences alone, however far from zero the logits are
+    rng = np.random.default_rng(vocab)
+    x = (rng.normal(size=(rows, vocab)) * 3 + offset).astype(np.float32)
+    ids = rng.integers(0, vocab, rows)
+    r = _logprobs(ctx, dtype, x, ids, 5)
+    ctx.sync()
+    _check_rows(r, ids, 5, dtype)
