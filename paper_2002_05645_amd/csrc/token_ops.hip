@@ -273,12 +273,14 @@ __device__ __forceinline__ uint32_t lanes_reach(uint32_t key, int count) {
   return reach;
 }
 
+// every logit is -inf (a NaN among them, which no maximum shows, is in the sum)
+__device__ __forceinline__ bool nothing(Stat st) { return st.m == -INFINITY && st.s == 0.f; }
 // log p of a logit x of the row
 __device__ __forceinline__ float log_prob(Stat st, float x) {
-  return st.m == -INFINITY ? -INFINITY : (x - st.m) - log2f(st.s) * LP_LN2;
+  return nothing(st) ? -INFINITY : (x - st.m) - log2f(st.s) * LP_LN2;
 }
 __device__ __forceinline__ void write_row(const LogprobArgs& a, int row, Stat st, int id, float x_id) {
-  const bool none = st.m == -INFINITY;   // every logit is -inf
+  const bool none = nothing(st);
   const float log_s = log2f(st.s);
   a.lse[row] = none ? -INFINITY : fmaf(log_s, LP_LN2, st.m);
   a.entropy[row] = none ? 0.f : (log_s - st.t / st.s) * LP_LN2;

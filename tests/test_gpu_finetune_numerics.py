@@ -86,3 +86,27 @@ def test_logprobs_do_not_depend_on_a_common_offset(ctx, dtype, offset, rows, voc
     r = _logprobs(ctx, dtype, x, ids, 5)
     ctx.sync()
     _check_rows(r, ids, 5, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("vocab", [3, 2000, 40001, 140000])
+def test_logprobs_of_rows_of_nan_are_nan(ctx, dtype, vocab):  # noqa: F811
+    # a model that has diverged: nothing but NaN, or NaN where the rest is masked away; it must not pass for a row without a possible token
+    x = np.random.default_rng(vocab).normal(size=(5, vocab)).astype(np.float32)
+    x[1] = np.nan
+    x[2] = -np.inf
+    x[2, vocab // 2] = np.nan
+    x[3] = -np.inf
+    ids = np.array([0, 1, 2, 1, 0])
+    g = torch.ones(5, device="cuda")
+    for work in (True, False):
+        r = _logprobs(ctx, dtype, x, ids, 2, work=work, g=g, h=g)
+        ctx.sync()
+        for name in ("logp", "entropy", "lse"):
+            got = to_host(r[name])
+            assert np.isnan(got[[1, 2]]).all() and np.isfinite(got[[0, 4]]).all(), name
+        assert to_host(r["lse"])[3] == -np.inf and to_host(r["logp"])[3] == -np.inf and to_host(r["entropy"])[3] == 0 and (r["dx"][3] == 0).all()
+        assert np.isnan(r["dx"][[1, 2]]).all() and np.isfinite(r["dx"][[0, 4]]).all()
+        assert np.isnan(to_host(r["top_logp"])[[1, 2]]).all()
+        top = r["top_ids"].cpu().numpy()
+        assert ((top >= 0) & (top < vocab)).all()
