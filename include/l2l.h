@@ -402,7 +402,8 @@ size_t l2l_op_dropout_work_bytes(int rows, int n);
 int l2l_op_token_logprobs(l2l_ctx*, int dtype, int rows, int vocab, const void* logits, long long ld, const int32_t* ids, float* logp,
                           float* entropy, float* lse, int top, int32_t* top_ids, float* top_logp, void* work);
 /* dlogits ([rows, vocab], row stride ldd, dtype of the logits; in place allowed) from the gradients of logp and of entropy (float [rows],
-   either may be NULL = zero); lse and entropy as the forward call left them.  Rows of nothing but -inf get zeros. */
+   either may be NULL = zero); lse and entropy as the forward call left them.  Rows of nothing but -inf get zeros.  Of rows whose |lse| is 256
+   (fp32) or 4096 (16-bit formats) or more, where its last bit is too coarse for log p, the logits are read twice. */
 int l2l_op_token_logprobs_bwd(l2l_ctx*, int dtype, int rows, int vocab, const void* logits, long long ld, const int32_t* ids, const float* lse,
                               const float* entropy, const float* dlogp, const float* dentropy, void* dlogits, long long ldd);
 size_t l2l_op_token_logprobs_work_bytes(int rows, int vocab, int top);

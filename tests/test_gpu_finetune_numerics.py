@@ -110,3 +110,32 @@ def test_logprobs_of_rows_of_nan_are_nan(ctx, dtype, vocab):  # noqa: F811
         assert np.isnan(to_host(r["top_logp"])[[1, 2]]).all()
         top = r["top_ids"].cpu().numpy()
         assert ((top >= 0) & (top < vocab)).all()
+
+
+@pytest.mark.parametrize("rows,vocab", [(5, 300), (5, 9001), (300, 40001), (5, 140000)])
+@pytest.mark.parametrize("dtype,fill,offset", [("fp32", "lowest", 0.0), ("fp32", -1e9, 0.0), ("bf16", "lowest", 0.0), ("bf16", -1e10, 0.0), ("fp16", "lowest", 0.0), ("fp32", -1e4, 3.0e4), ("fp32", -1e4, 290.0),
+                                               ("fp32", -1e4, 200.0), ("bf16", -1e4, 3.0e4), ("fp16", -6e4, -5.0e3), ("bf16", -1e4, 2.0e3)])
+def test_logprob_gradients_of_masked_and_far_rows(ctx, dtype, fill, offset, rows, vocab):  # noqa: F811
+    # lse alone does not hold log p of a row whose logits are all far from zero (a row of nothing but the mask is one)
+    x, ids = _masked_rows(dtype, fill, rows, vocab)
+    x = np.where(x > -5e3, x + np.float32(offset), x).astype(np.float32)
+    g, h = torch.randn(rows, device="cuda"), torch.randn(rows, device="cuda")
+    gh, hh = to_host(g)[:, None], to_host(h)[:, None]
+    for ld, in_place in ((vocab, False), (vocab + 5, True)):
+        r = _logprobs(ctx, dtype, x, ids, 6, ld, True, g, h, in_place)
+        ctx.sync()
+        if not in_place:
+            _check_rows(r, ids, 6, dtype)
+            xs = r["x"]
+            _, entropy, lse, _, _, lp = _row_reference(xs, ids, 0)
+            p = np.exp(lp)
+            ref = -p * (gh + hh * (np.where(p > 0, lp, 0.0) + entropy[:, None]))
+            ref[np.arange(rows), ids] += gh[:, 0]
+            near = np.minimum(np.where(np.isfinite(xs), xs.max(-1, keepdims=True) - xs, 0.0), 104.0).max(-1)
+            f = (96 + 4 * near) * E24
+            # what the last bit of an lse up to 256 (fp32) or 4096 (16-bit formats) leaves open in log p
+            left = np.minimum(np.abs(lse), 256.0 if dtype == "fp32" else 4096.0) * E24
+            size = np.abs(gh) + np.abs(hh) * (near + 2 * np.log(vocab) + 2)[:, None]
+            tol = (U[dtype] + 2 * E24) * np.abs(ref) + (8 * f + 4 * left)[:, None] * p * size + LOW[dtype]
+        err = np.abs(r["dx"] - ref)
+        assert (err <= tol).all(), (in_place, (err / tol).max())
