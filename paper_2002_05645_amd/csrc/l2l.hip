@@ -1643,10 +1643,10 @@ int l2l_sync(l2l_ctx* c) {
     HIP_TRY(c, hipMemcpy(&bad, c->bad_ids, 4, hipMemcpyDeviceToHost));
     if (bad) {
       HIP_TRY(c, hipMemset(c->bad_ids, 0, 4));
-      if (bad == 2)
-        return fail(c, L2L_E_ARG, "l2l_op_attention: a sequence that does not fit the token rows or max_len was passed since the last l2l_sync; such sequences are skipped");
-      return fail(c, L2L_E_ARG, "a token id or label outside its range (vocabulary %d, or the head's classes) was passed since the last l2l_sync; such ids are clamped and the results are not meaningful",
-                  c->cfg.vocab);
+      const char* sequence = bad & 2 ? "l2l_op_attention: a sequence that does not fit the token rows or max_len was passed since the last l2l_sync; such sequences are skipped" : "";
+      if (!(bad & 1)) return fail(c, L2L_E_ARG, "%s", sequence);
+      return fail(c, L2L_E_ARG, "a token id or label outside its range (vocabulary %d, or the head's classes) was passed since the last l2l_sync; such ids are clamped and the results are not meaningful%s%s",
+                  c->cfg.vocab, bad & 2 ? "; " : "", sequence);
     }
   }
   return L2L_OK;

@@ -139,3 +139,27 @@ def test_logprob_gradients_of_masked_and_far_rows(ctx, dtype, fill, offset, rows
             tol = (U[dtype] + 2 * E24) * np.abs(ref) + (8 * f + 4 * left)[:, None] * p * size + LOW[dtype]
         err = np.abs(r["dx"] - ref)
         assert (err <= tol).all(), (in_place, (err / tol).max())
+
+
+# ------------------------------------------------------------------------------------- what l2l_sync reports
+def test_sync_names_every_kind_of_bad_input(ctx):  # noqa: F811
+    x = Problem("bf16", 2, 2, 64, [40, 50], seed=8)
+    plan = P.make_attention(dtype="bf16", heads=2, head_dim=64, sequences=2, max_len=50, rows=x.rows, first=dev_i32([0, x.rows - 10]), length=dev_i32([40, 50]))
+    logits = torch.randn(3, 100, device="cuda")
+    out = [torch.empty(3, device="cuda") for _ in range(3)]
+
+    def sequence():
+        ctx.op_attention(plan, x.q, x.q.stride(0), x.k, x.k.stride(0), x.v, x.v.stride(0), x.o, x.o.stride(0))
+
+    def token():
+        ctx.op_token_logprobs(P.L2L_F32, 3, 100, logits, 100, dev_i32([1, 100, 2]), *out)
+    for calls, named, not_named in (((sequence,), "sequence that does not fit", "token id"), ((token,), "token id", "sequence that does not fit"), ((sequence, token), None, None)):
+        for call in calls:
+            call()
+        with pytest.raises(P.L2LError) as e:
+            ctx.sync()
+        if named:
+            assert named in str(e.value) and not_named not in str(e.value)
+        else:
+            assert "sequence that does not fit" in str(e.value) and "token id" in str(e.value)
+        ctx.sync()
