@@ -2403,7 +2403,7 @@ static AttentionSplits attention_plan(const l2l_attention* a) {
     if (attention_in_one(a)) p.dkv = attention_head_splits((double)a->sequences * a->kv_heads, group, tiles, 2 * kv * a->head_dim * 4);
     else p.dkv = attention_splits(blocks * a->kv_heads, tiles * group, total, us, 2 * kv * a->head_dim * 4);
   }
-  if (p.fwd > 1) p.fwd_bytes = (size_t)(p.fwd * q * (a->head_dim + 1)) * 4;
+  if (p.fwd > 1) p.fwd_bytes = (size_t)(p.fwd * q * (a->head_dim + 2)) * 4;
   p.bwd_bytes = stats + (size_t)std::max(p.dq > 1 ? p.dq * q * a->head_dim * 4 : 0.0, p.dkv > 1 ? p.dkv * 2 * kv * a->head_dim * 4 : 0.0);
   return p;
 }
@@ -2471,7 +2471,8 @@ int l2l_op_attention(l2l_ctx* c, const l2l_attention* a, const void* q, long lon
   g.out = o; g.ldo = ldo; g.lse = lse;
   g.splits_fwd = work ? attention_plan(a).fwd : 1;
   g.part = (float*)work;
-  g.part_lse = g.part + (long long)g.splits_fwd * a->rows * a->heads * a->head_dim;
+  g.part_m = g.part + (long long)g.splits_fwd * a->rows * a->heads * a->head_dim;
+  g.part_sum = g.part_m + (long long)g.splits_fwd * a->rows * a->heads;
   return timed(c, L2L_PROF_ATTN, 0, 0, [&] { L2L_SEQ_ATTN_PICK(fwd, a->dtype, a->head_dim, g, c->cs); });
 }
 

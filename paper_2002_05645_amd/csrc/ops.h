@@ -24,7 +24,7 @@ struct SeqAttnArgs {
   int splits_fwd, splits_dq, splits_dkv;
   int in_one;                         // backward: one kernel for all three gradients; splits_dkv then divides the query heads of a key head
   float* part;                        // [split][rows][heads d]; dK / dV: [split][2][rows][kv_heads d], dV first
-  float* part_lse;                    // forward: [split][heads][rows]
+  float *part_m, *part_sum;           // forward, [split][heads][rows]: the maximum (of the scores before their scale) and the sum that a part's rows are relative to
   int by_group;                       // 1: an XCD takes the query heads that share a key head one after the other
   int32_t* bad;                       // bit 1: a sequence did not fit rows or max_len
 };

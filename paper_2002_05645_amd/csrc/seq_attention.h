@@ -262,10 +262,9 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
   const float kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
   const float l = half_sum(sum);
   if (a.splits_fwd > 1) {   // (a split without a key that the row sees: l = 0)
-    const bool none = l == 0.f;
-    const long long row = (long long)split * a.rows + sq.first + q;
-    store_part<DP>(o, a.part + row * ((long long)a.heads * a.d) + (long long)h * a.d, q < n, a.d, lane, none ? 0.f : kept / l);
-    if (lane < 32 && q < n) a.part_lse[((long long)split * a.heads + h) * a.rows + sq.first + q] = none ? -INFINITY : (m * c + __builtin_amdgcn_logf(l)) * LN2;
+    const long long row = (long long)split * a.rows + sq.first + q, stat = ((long long)split * a.heads + h) * a.rows + sq.first + q;
+    store_part<DP>(o, a.part + row * ((long long)a.heads * a.d) + (long long)h * a.d, q < n, a.d, lane, l == 0.f ? 0.f : kept / l);
+    if (lane < 32 && q < n) { a.part_m[stat] = m; a.part_sum[stat] = l; }
     return;
   }
   store_rows<E, DP>(o, lds + wave * I::IMG, (E*)a.out + (sq.first + q0) * a.ldo + (long long)h * a.d, a.ldo, n - q0, a.d, lane, kept / l);
@@ -654,12 +653,13 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
 }
 
 // ---- partial results of the splits together -------------------------------------------------------------------------------
-// out = sum over the splits of part, or with WEIGHTED (forward) of e^(lse_s - lse) part_s, lse = log sum e^lse_s.  A workgroup takes 64
-// rows of one (sequence, head), eight columns a thread; splits in their order.  Bound by memory, the splits' share of it.
+// out = sum over the splits of part, or with WEIGHTED (forward) of w_s part_s / sum w with w_s = sum_s e^(scale (m_s - m)), from the maxima and sums
+// themselves (weights from an lse per split would carry its last bit, 2^-24 of the score, into O).  A workgroup takes 64 rows of one
+// (sequence, head), eight columns a thread; splits in their order.  Bound by memory, the splits' share of it.
 struct JoinArgs {
   const float* part[2];     // of dV and dK; otherwise one
   long long split_stride;   // elements from a split to the next
-  const float* part_lse;    // WEIGHTED
+  const float *part_m, *part_sum;   // WEIGHTED
   float* lse;               // WEIGHTED: or null
   void* out[2];
   long long ldo[2];
@@ -679,27 +679,27 @@ __global__ __launch_bounds__(256) void seq_join_kernel(const SeqAttnArgs a, cons
     const long long row = sq.first + i, at = row * ((long long)j.heads * a.d) + (long long)h * a.d + col;
     // four splits' loads at a time, without a branch between them: places past the last split are read again and count nothing
     float top = -INFINITY, total = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const auto lse_of = [&](int s) { return j.part_lse[((long long)min(s, j.splits - 1) * j.heads + h) * a.rows + row]; };
+    const auto stat_of = [&](const float* stat, int s) { return stat[((long long)min(s, j.splits - 1) * j.heads + h) * a.rows + row]; };
     if (WEIGHTED) {
       for (int s0 = 0; s0 < j.splits; s0 += 4) {
-        float l[4];
+        float m[4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) l[x] = lse_of(s0 + x);
-        top = fmaxf(fmaxf(top, fmaxf(l[0], l[1])), fmaxf(l[2], l[3]));
+        for (int x = 0; x < 4; ++x) m[x] = stat_of(j.part_m, s0 + x);
+        top = fmaxf(fmaxf(top, fmaxf(m[0], m[1])), fmaxf(m[2], m[3]));
       }
     }
     for (int s0 = 0; s0 < j.splits; s0 += 4) {
-      float v[4][8], w[4];
+      float v[4][8], m[4], w[4];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         load8(part + min(s0 + x, j.splits - 1) * j.split_stride + at, v[x]);
-        w[x] = WEIGHTED ? lse_of(s0 + x) : 0.f;
+        if (WEIGHTED) { m[x] = stat_of(j.part_m, s0 + x); w[x] = stat_of(j.part_sum, s0 + x); }
       }
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         if (s0 + x >= j.splits) continue;
         if (WEIGHTED) {
-          w[x] = w[x] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((w[x] - top) * LOG2E);   // (-inf: a split without a key that the row sees)
+          if (w[x] != 0.f) w[x] *= __builtin_amdgcn_exp2f((m[x] - top) * (a.scale * LOG2E));   // (0: a split without a key that the row sees)
           total += w[x];
         }
 #pragma unroll
@@ -709,7 +709,7 @@ __global__ __launch_bounds__(256) void seq_join_kernel(const SeqAttnArgs a, cons
     if (WEIGHTED) {
 #pragma unroll
       for (int x = 0; x < 8; ++x) acc[x] /= total;
-      if (j.lse && col == 0) j.lse[(long long)h * a.rows + row] = top + __builtin_amdgcn_logf(total) * LN2;
+      if (j.lse && col == 0) j.lse[(long long)h * a.rows + row] = fmaf(top, a.scale, __builtin_amdgcn_logf(total) * LN2);
     }
     store8(out + row * ldo + (long long)h * a.d + col, acc);
   }

@@ -191,10 +191,9 @@ __global__ __launch_bounds__(256) void seq_fwd_f32_kernel(const SeqAttnArgs a) {
   const float l = half_sum(sum), kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
   if (q >= n) return;
   if (a.splits_fwd > 1) {   // (a split without a key that the row sees: l = 0)
-    const bool none = l == 0.f;
-    const long long row = (long long)split * a.rows + sq.first + q;
-    I::store(o, a.part + row * ((long long)a.heads * a.d) + (long long)h * a.d, a.d, lane, none ? 0.f : kept / l);
-    if (lane < 32) a.part_lse[((long long)split * a.heads + h) * a.rows + sq.first + q] = none ? -INFINITY : m * a.scale + __builtin_amdgcn_logf(l) * LN2;
+    const long long row = (long long)split * a.rows + sq.first + q, stat = ((long long)split * a.heads + h) * a.rows + sq.first + q;
+    I::store(o, a.part + row * ((long long)a.heads * a.d) + (long long)h * a.d, a.d, lane, l == 0.f ? 0.f : kept / l);
+    if (lane < 32) { a.part_m[stat] = m; a.part_sum[stat] = l; }
     return;
   }
   I::store(o, (float*)a.out + (sq.first + q) * a.ldo + (long long)h * a.d, a.d, lane, kept / l);

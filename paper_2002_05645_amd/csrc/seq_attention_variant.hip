@@ -33,15 +33,15 @@ void join(const SeqAttnArgs& a, const sattn::JoinArgs& j, hipStream_t s) {
   hipLaunchKernelGGL((sattn::seq_join_kernel<Elem, WEIGHTED>), grid, dim3(256), 0, s, a, j);
 }
 void join_fwd(const SeqAttnArgs& a, hipStream_t s) {
-  if (a.splits_fwd > 1) join<true>(a, {{a.part}, a.rows * a.heads * a.d, a.part_lse, a.lse, {a.out}, {a.ldo}, a.splits_fwd, a.heads}, s);
+  if (a.splits_fwd > 1) join<true>(a, {{a.part}, a.rows * a.heads * a.d, a.part_m, a.part_sum, a.lse, {a.out}, {a.ldo}, a.splits_fwd, a.heads}, s);
 }
 void join_dq(const SeqAttnArgs& a, hipStream_t s) {
-  if (a.splits_dq > 1) join<false>(a, {{a.part}, a.rows * a.heads * a.d, nullptr, nullptr, {a.dq}, {a.lddq}, a.splits_dq, a.heads}, s);
+  if (a.splits_dq > 1) join<false>(a, {{a.part}, a.rows * a.heads * a.d, nullptr, nullptr, nullptr, {a.dq}, {a.lddq}, a.splits_dq, a.heads}, s);
 }
 void join_dkv(const SeqAttnArgs& a, hipStream_t s) {
   const long long one = a.rows * a.kv_heads * a.d;
   if (a.splits_dkv > 1)
-    join<false>(a, {{a.part, a.part + one}, 2 * one, nullptr, nullptr, {a.dv, a.dk}, {a.lddv, a.lddk}, a.splits_dkv, a.kv_heads}, s);
+    join<false>(a, {{a.part, a.part + one}, 2 * one, nullptr, nullptr, nullptr, {a.dv, a.dk}, {a.lddv, a.lddk}, a.splits_dkv, a.kv_heads}, s);
 }
 
 template <typename K>

@@ -163,3 +163,106 @@ def test_sync_names_every_kind_of_bad_input(ctx):  # noqa: F811
         else:
             assert "sequence that does not fit" in str(e.value) and "token id" in str(e.value)
         ctx.sync()
+
+
+# ------------------------------------------------------------------------------------- attention
+def _plan(x, causal, scale):
+    return P.make_attention(dtype=x.dtype, heads=x.heads, kv_heads=x.kv, head_dim=x.d, sequences=len(x.lengths), max_len=max(x.lengths), rows=x.rows, first=dev_i32(x.first),
+                            length=dev_i32(x.lengths), causal=causal, scale=scale)
+
+
+def _check_large_scores(x, causal, scale):
+    """o, lse, dq, dk, dv, entry by entry, where what bounds the error is the scores' own size: a sum of d products rounds d times, by up to 2^-24 of
+    the products' magnitudes together each, which is an absolute error of the score and a relative one of P"""
+    host = {m: to_host(getattr(x, m)) for m in ("q", "k", "v", "do", "o", "dq", "dk", "dv", "lse")}
+    d, u, G, low = x.d, U[x.dtype], x.heads // x.kv, LOW[x.dtype]
+    uP = 0.0 if x.dtype == "fp32" else u
+    for b, n in enumerate(x.lengths):
+        r = slice(x.first[b], x.first[b] + n)
+        for hk in range(x.kv):
+            ck = slice(hk * d, hk * d + d)
+            k, v = host["k"][r, ck], host["v"][r, ck]
+            total = dict(dk=0, dv=0, dk_tol=0, dv_tol=0)
+            for h in range(hk * G, hk * G + G):
+                c = slice(h * d, h * d + d)
+                q, do = host["q"][r, c], host["do"][r, c]
+                o, lse, prob = F.attention(q, k, v, scale, causal, 1.0)
+                dq, dk, dv, dS = F.attention_bwd(q, k, v, scale, 1.0, prob, do)
+                e = (d + 4) * E24 * scale * (np.abs(q) @ np.abs(k).T).max()      # of a score
+                lse_tol = e + (n + 32 + 2 * np.abs(lse)) * E24
+                assert (np.abs(host["lse"][h, r] - lse) <= lse_tol).all(), ("lse", b, h)
+                f = 2 * e + (n + d + 32) * E24                                    # of P in the forward pass: its score and its row's sum
+                fb = 2 * e + (n + 2 * d + 32) * E24 + (d / 2 + 4) * np.abs(lse).max() * E24      # in the backward pass: its score, lse and sums that begin at lse
+                o_in = (uP + f) * (prob @ np.abs(v)) + n * low * np.abs(v).max()
+                o_tol = o_in + u * (np.abs(o) + o_in) + low
+                assert (np.abs(host["o"][r, c] - o) <= o_tol).all(), ("o", b, h)
+                D = (np.abs(do) * np.abs(o)).sum(-1)[:, None]
+                dP = np.abs(do) @ np.abs(v).T
+                dS_tol = (uP + fb) * np.abs(dS) + prob * ((np.abs(do) * o_tol).sum(-1)[:, None] + fb * (dP + D)) * (1 + u) + low
+                dq_tol = scale * (dS_tol @ np.abs(k)) + scale * n * E24 * (np.abs(dS) @ np.abs(k))
+                dq_tol = dq_tol + u * (np.abs(dq) + dq_tol) + low
+                assert (np.abs(host["dq"][r, c] - dq) <= dq_tol).all(), ("dq", b, h)
+                total["dk"] += dk
+                total["dv"] += dv
+                total["dk_tol"] += scale * (dS_tol.T @ np.abs(q)) + scale * G * n * E24 * (np.abs(dS).T @ np.abs(q))
+                total["dv_tol"] += (uP + fb + G * n * E24) * (prob.T @ np.abs(do)) + n * low * np.abs(do).max()
+            for name in ("dk", "dv"):
+                tol = total[name + "_tol"]
+                assert (np.abs(host[name][r, ck] - total[name]) <= tol + u * (np.abs(total[name]) + tol) + low).all(), (name, b, hk)
+
+
+@pytest.mark.parametrize("scale", [4.0, 64.0])
+@pytest.mark.parametrize("dtype,d,lengths", [("bf16", 64, [200, 33, 2]), ("fp16", 96, [200, 33, 2]), ("fp32", 64, [200, 33, 2]), ("bf16", 128, [1300]), ("fp32", 32, [1300]), ("fp16", 64, [100, 128, 1])])
+def test_attention_of_large_scores(ctx, dtype, d, lengths, scale):  # noqa: F811
+    # scores of hundreds and thousands, rows that one workgroup adds up and rows in parts
+    x = Problem(dtype, 2, 1, d, lengths, True, 0.0, seed=3)
+    x.plan = _plan(x, True, scale)
+    x.forward(ctx)
+    x.backward(ctx)
+    ctx.sync()
+    _check_large_scores(x, True, scale)
+
+
+def _means_over_the_largest(x, causal, scale):
+    """q and k are whole numbers and a score is at least a thousand times the next one off: o is the mean of v over a row's largest scores"""
+    o, lse, d, G = to_host(x.o), to_host(x.lse), x.d, x.heads // x.kv
+    for b, n in enumerate(x.lengths):
+        r = slice(x.first[b], x.first[b] + n)
+        for h in range(x.heads):
+            c, ck = slice(h * d, h * d + d), slice(h // G * d, h // G * d + d)
+            s, v = to_host(x.q[r, c]) @ to_host(x.k[r, ck]).T, to_host(x.v[r, ck])
+            if causal:
+                s = np.where(np.tril(np.ones((n, n), bool)), s, -np.inf)
+            top = s.max(-1)
+            best = s == top[:, None]
+            count = best.sum(-1)
+            ref = (best @ v) / count[:, None]
+            # a mean of n terms at most in fp32, then rounded to the format
+            tol = U[x.dtype] * np.abs(ref) + (n + 8) * E24 * ((best @ np.abs(v)) / count[:, None]) * (1 + U[x.dtype]) + LOW[x.dtype]
+            assert (np.abs(o[r, c] - ref) <= tol).all(), (causal, b, h)
+            ref = scale * top + np.log(count)
+            assert (np.abs(lse[h, r] - ref) <= 4 * E24 * np.abs(ref) + 8 * E24 * np.log(n + 1)).all(), (causal, b, h)
+
+
+def _whole_numbers(dtype, d, lengths, amount, scale):
+    """a Problem with scores that fp32 holds exactly, ties among them"""
+    x = Problem(dtype, 2, 1, d, lengths, False, 0.0, seed=d + len(lengths))
+    g = torch.Generator().manual_seed(d)
+    mine = torch.from_numpy(x.mine).cuda()
+    x.qkv[mine, :3 * d] = torch.randint(-amount, amount + 1, (sum(lengths), 3 * d), generator=g).to(TDT[dtype]).cuda()
+    x.plan = _plan(x, False, scale)
+    return x
+
+
+def _parts_with_ties(ctx, dtype, lengths):  # noqa: F811
+    x = _whole_numbers(dtype, 32, lengths, 1, 1024.0)
+    assert x.work.numel() >= 2 * x.rows * 8 + 2 * 2 * x.rows * 32 * 4      # (rows in parts)
+    x.forward(ctx)
+    ctx.sync()
+    _means_over_the_largest(x, False, 1024.0)
+
+
+@pytest.mark.parametrize("lengths", [[1300], [700, 2, 901]])
+def test_attention_rows_in_parts_keep_ties(ctx, lengths):  # noqa: F811
+    # equal scores of some ten thousand in different parts of a row have equal weights
+    _parts_with_ties(ctx, "fp32", lengths)
