@@ -26,6 +26,7 @@ using attn::pack8;
 using attn::zero16;
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float NEAR = 1024.f;   // scores, in powers of two, whose products may be rounded (by 2^-15 at most) before their differences are taken
 
 // over lanes l and l ^ 32 (the swap leaves the lower half's values in one register and the upper half's in the other)
 struct Halves { float lo, hi; };
@@ -188,9 +189,10 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
   if (from < tiles) fetch(from);
   bf16x8 qf[DP / 16];
   f32x16 o[DP / 32];
-  // No maximum yet: far below any score, and finite, as a split's first tile may have no key that the row sees.
+  // No maximum yet: below any score, and finite with its product, as a split's first tile may have no key that the row sees.
   const float c = a.scale * LOG2E;
-  float m = fmaxf(-1e30f / c, -1e38f), sum = 0.f;
+  float m = -3e38f / fmaxf(c, 1.0f), sum = 0.f;
+  bool far = false;   // a maximum of the wave's rows is not near
   I::template row_frags<E>((const E*)a.q + (sq.first + q) * a.ldq + (long long)h * a.d, q < n, a.d, lane, qf);
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t) o[t] = zero16();
@@ -223,13 +225,20 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
       if (__any((cm - m) * c > 8.0f)) {
         const float rescale = __builtin_amdgcn_exp2f((m - cm) * c);   // 0 on the first tile
         m = cm;
+        far = __any(fabsf(m * c) > NEAR);
         sum *= rescale;
 #pragma unroll
         for (int t2 = 0; t2 < DP / 32; ++t2)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[t2][r] *= rescale;
       }
-      const float mc = m * c;
+      // Near zero one fma a score, whose second product is rounded; far from it the difference first: half a step of m c, a factor of
+      // every P of the row, is 2^128 where m c is 2^31.
+      if (far) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] -= m;
+      }
+      const float mc = far ? 0.f : m * c;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -mc));
@@ -260,15 +269,16 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
   __syncthreads();   // the images are no longer read: a quarter of them is each wave's way out
   if (!active) return;
   const float kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
-  const float l = half_sum(sum);
+  const float l = half_sum(sum), mc = m * c;
+  const float rest = fabsf(mc) <= NEAR ? fmaf(m, c, -mc) : 0.f;   // (what the rounded product left out, in l)
   if (a.splits_fwd > 1) {   // (a split without a key that the row sees: l = 0)
     const long long row = (long long)split * a.rows + sq.first + q, stat = ((long long)split * a.heads + h) * a.rows + sq.first + q;
     store_part<DP>(o, a.part + row * ((long long)a.heads * a.d) + (long long)h * a.d, q < n, a.d, lane, l == 0.f ? 0.f : kept / l);
-    if (lane < 32 && q < n) { a.part_m[stat] = m; a.part_sum[stat] = l; }
+    if (lane < 32 && q < n) { a.part_m[stat] = m; a.part_sum[stat] = l * __builtin_amdgcn_exp2f(-rest); }
     return;
   }
   store_rows<E, DP>(o, lds + wave * I::IMG, (E*)a.out + (sq.first + q0) * a.ldo + (long long)h * a.d, a.ldo, n - q0, a.d, lane, kept / l);
-  if (a.lse && lane < 32 && q < n) a.lse[(long long)h * a.rows + sq.first + q] = (m * c + __builtin_amdgcn_logf(l)) * LN2;
+  if (a.lse && lane < 32 && q < n) a.lse[(long long)h * a.rows + sq.first + q] = fmaf(m, a.scale, (__builtin_amdgcn_logf(l) - rest) * LN2);
 }
 
 // ---- dQ, and what the dK / dV kernel needs of each row ----------------------------------------------------------------

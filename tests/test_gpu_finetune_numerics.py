@@ -266,3 +266,43 @@ def _parts_with_ties(ctx, dtype, lengths):  # noqa: F811
 def test_attention_rows_in_parts_keep_ties(ctx, lengths):  # noqa: F811
     # equal scores of some ten thousand in different parts of a row have equal weights
     _parts_with_ties(ctx, "fp32", lengths)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("lengths", [[1300], [700, 2, 901]])
+def test_attention_rows_in_parts_keep_ties_in_16_bits(ctx, dtype, lengths):  # noqa: F811
+    _parts_with_ties(ctx, dtype, lengths)
+
+
+@pytest.mark.parametrize("dtype,d,lengths", [("bf16", 64, [200, 33, 2]), ("fp16", 64, [200, 33, 2]), ("fp32", 64, [200, 33, 2]), ("bf16", 128, [1300]), ("fp16", 96, [1300]), ("fp32", 32, [1300]),
+                                             ("bf16", 64, [100, 128, 1]), ("fp16", 32, [100, 128, 1]), ("fp32", 64, [60, 33, 1])])
+@pytest.mark.parametrize("amount", [2, 200])
+def test_attention_forward_of_scores_of_any_size(ctx, dtype, d, lengths, amount):  # noqa: F811
+    # scores of up to 2^18 and 2^32; the products of a score and its scale are beyond what their last bits may be a factor of
+    for causal in (False, True):
+        x = _whole_numbers(dtype, d, lengths, amount, 1024.0)
+        x.plan = _plan(x, causal, 1024.0)
+        x.forward(ctx)
+        ctx.sync()
+        _means_over_the_largest(x, causal, 1024.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n", [90, 700])
+def test_attention_forward_of_scores_far_below_zero(ctx, dtype, n):  # noqa: F811
+    # every score of a row beyond -1e30: the least of them have all of the probability
+    d = 64
+    x = Problem(dtype, 1, 1, d, [n], False, 0.0, seed=5)
+    mine = torch.arange(n, device="cuda") + x.first[0]
+    step = torch.randperm(n, generator=torch.Generator().manual_seed(n)).cuda().float() // 128 + 1.0      # a few distinct sizes, so ties
+    x.q[mine] = torch.full((n, d), 2.0 ** 52, device="cuda").to(TDT[dtype])
+    x.k[mine] = (-(2.0 ** 52) * step)[:, None].expand(n, d).to(TDT[dtype])
+    x.forward(ctx)
+    ctx.sync()
+    best = (step == 1).cpu().numpy()
+    v = to_host(x.v[mine])
+    ref = v[best].mean(0)
+    tol = U[dtype] * np.abs(ref) + (n + 8) * E24 * np.abs(v[best]).mean(0) * (1 + U[dtype])
+    assert (np.abs(to_host(x.o[mine]) - ref) <= tol).all()
+    score = -(2.0 ** 104) * d * d ** -0.5
+    assert (np.abs(to_host(x.lse[0, mine]) - score) <= 4 * E24 * abs(score)).all()
