@@ -357,7 +357,7 @@ typedef struct {
   const int32_t* first;
   const int32_t* len;
   int causal;            /* 1: a query sees the keys up to its own position; 0: all of its sequence */
-  float scale;           /* 2^-64 to 2^64: factor on the scores, 1 / sqrt(d) as a rule */
+  float scale;           /* 2^-64 to 2^10: factor on the scores, 1 / sqrt(d) as a rule */
   double dropout;        /* share of the probabilities that is dropped (the others are divided by the kept share); to the
                             nearest 1/256, one random byte a probability: byte 4 (i % 4) + j % 4 of the call with counter words 0, 1 =
                             (i / 4) << 16 | j / 4, 2^31 | (b heads + h) for query i, key j of sequence b and head h is kept if >= 256 p */
@@ -373,7 +373,8 @@ int l2l_op_attention(l2l_ctx*, const l2l_attention*, const void* q, long long ld
                      void* o, long long ldo, float* lse, void* work);
 /* Its gradients: dq [rows, heads d], dk, dv [rows, kv_heads d] (summed over the query heads that share them) from dout, the
    gradient of o.  q, k, v, o, lse and the description as in the forward call; the probabilities are computed
-   again.  No atomics: the same call gives the same bits.  Outputs must not overlap inputs.  work: required. */
+   again, from lse, whose last bit counts: their relative error reaches 2^-21 of the largest |score| (a 16-bit format's half step at scores of some
+   thousands; scores of 2^20 and more leave gradients without a meaning, and from 2^27 on they may be NaN).  No atomics: the same call gives the same bits.  Outputs must not overlap inputs.  work: required. */
 int l2l_op_attention_bwd(l2l_ctx*, const l2l_attention*, const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv,
                          const void* o, long long ldo, const float* lse, const void* dout, long long lddo, void* dq, long long lddq,
                          void* dk, long long lddk, void* dv, long long lddv, void* work);

@@ -2344,7 +2344,7 @@ static const char* attention_desc_error(const l2l_attention* a) {
   if (a->head_dim < 8 || a->head_dim > 128 || a->head_dim % 8) return "head_dim must be a multiple of 8 from 8 to 128";
   if (a->sequences < 0 || a->rows < 0 || a->max_len < 0 || a->max_len > 262144) return "sequences, rows and max_len (at most 262144) must not be negative";
   if (!a->first && (long long)a->sequences * a->max_len > a->rows) return "without `first`, sequences x max_len must not exceed rows";
-  if (!(a->scale >= 0x1p-64f && a->scale <= 0x1p64f)) return "scale must be positive and finite, from 2^-64 to 2^64";
+  if (!(a->scale >= 0x1p-64f && a->scale <= 0x1p10f)) return "scale must be from 2^-64 to 2^10";
   if (!drop_threshold(a->dropout, 256, &drop)) return "dropout must be 0, or from 1/512 to 511/512 (it is taken to the nearest 1/256)";
   if (((uintptr_t)a->first | (uintptr_t)a->len) & 3 || (uintptr_t)a->step & 7) return "misaligned first, len or step";
   if ((long long)a->sequences * a->heads * ((a->max_len + 127) / 128) > (1LL << 23)) return "too many (sequence, head, query block)s for one launch";
