@@ -2387,10 +2387,12 @@ static int attention_head_splits(double wgs, int group, int tiles, double bytes)
 struct AttentionSplits { int fwd, dq, dkv; size_t fwd_bytes, bwd_bytes; };   // bytes of workspace of either call
 // the backward pass in one kernel: a workgroup has all of a head's keys (wider heads leave no registers for it)
 static bool attention_in_one(const l2l_attention* a) { return is16(a->dtype) && a->max_len <= 128 && a->head_dim <= 64; }
+// floats of a row and head that the backward kernels leave each other (fp16 in two kernels: its bounds too)
+static int attention_row_stats(const l2l_attention* a) { return a->dtype == L2L_FP16 && !attention_in_one(a) ? 3 : 2; }
 static AttentionSplits attention_plan(const l2l_attention* a) {
   AttentionSplits p = {1, 1, 1, 0, 0};
   const double rows = (double)a->rows, q = rows * a->heads, kv = rows * a->kv_heads;
-  const size_t stats = ((size_t)(2 * q) * 4 + 15) / 16 * 16;
+  const size_t stats = ((size_t)(attention_row_stats(a) * q) * 4 + 15) / 16 * 16;
   if (a->max_len > 0 && a->sequences > 0) {
     // How long the sequences really are only the device knows: max_len and the token rows bound them.
     const int tiles = (a->max_len + 63) / 64, group = a->heads / a->kv_heads;
@@ -2499,7 +2501,8 @@ int l2l_op_attention_bwd(l2l_ctx* c, const l2l_attention* a, const void* q, long
   g.in_one = attention_in_one(a); g.splits_dq = p.dq; g.splits_dkv = p.dkv;
   g.nlse2 = (float*)work;
   g.delta = g.nlse2 + (long long)a->heads * a->rows;
-  g.part = g.nlse2 + (2 * (long long)a->heads * a->rows + 3) / 4 * 4;
+  g.bounds = (uint32_t*)(g.delta + (long long)a->heads * a->rows);
+  g.part = g.nlse2 + (attention_row_stats(a) * (long long)a->heads * a->rows + 3) / 4 * 4;
   return timed(c, L2L_PROF_ATTN, 0, 0, [&] { L2L_SEQ_ATTN_PICK(bwd, a->dtype, a->head_dim, g, c->cs); });
 }
 

@@ -11,6 +11,7 @@ struct SeqAttnArgs {
   float* lse;                         // [heads][rows]; written forward, read backward
   float* nlse2;                       // backward, [heads][rows]: -lse / scale (16-bit formats) ...
   float* delta;                       // ... and rowsum(dO O) (16-bit formats: negated), left by the dQ kernel for the dK / dV kernel
+  uint32_t* bounds;                   // backward in fp16 by two kernels, [heads][rows]: at the first of each 32 rows of a sequence their largest kept |dO| (low half, as bf16) and |D|
   long long ldq, ldk, ldv, ldo, lddo, lddq, lddk, lddv;   // row strides in elements
   const int32_t *first, *len;         // device, per sequence, or null
   int heads, kv_heads, d, sequences, max_len, causal;

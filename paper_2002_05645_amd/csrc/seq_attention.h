@@ -140,6 +140,32 @@ struct Tiles {
     for (int i = 0; i < PER; ++i) lds_load16(from, off[i], to + wave * 1024 + i * 4096);
   }
 };
+// fp16 ends at 6e-5 below (6e-8 with few bits), where bf16 has the range of fp32; the dS of a long row is smaller than dO by its length.  P and dS of the backward
+// kernels are therefore taken times 2^up, a power for each lane, whose row or key all of its accumulators belong to: UP_MOST, which keeps P in
+// range, until a dS outgrows it (dQ kernel), or less from the start by dS's bound, the largest |dO| |v| + |D| (dK / dV kernel, which knows both and
+// whose registers leave no room for a look at every dS).  (3000 keys, dO of 1e-3: dQ off by 3.9e-3 of its norm without, 6e-4 with, which is its own rounding.)
+constexpr float UP_MOST = 14.f, UP_LIMIT = 32768.f;
+// the power of two to take a number beyond UP_LIMIT down by, with two bits to spare (infinity: by all there is)
+__device__ __forceinline__ float power_down(float x, float up) {
+  const float by = (float)((int)(__builtin_bit_cast(uint32_t, x) >> 23) - (127 + 12));
+  return x > UP_LIMIT ? fminf(by, up) : 0.f;
+}
+// the largest of 32 rows' kept |dO| and |D|, rounded up to 16 bits each
+__device__ __forceinline__ uint32_t pack_bounds(float norm, float D) {
+  const uint32_t a = __builtin_bit_cast(uint32_t, wave_max(norm)) + 0xFFFFu, b = __builtin_bit_cast(uint32_t, wave_max(fabsf(D))) + 0xFFFFu;
+  return (a >> 16) | (b & 0xFFFF0000u);
+}
+__device__ __forceinline__ float largest16(const f32x16& g) {
+  float x = fabsf(g[0]);
+#pragma unroll
+  for (int r = 1; r < 16; ++r) x = fmaxf(x, fabsf(g[r]));
+  return x;
+}
+template <int N>
+__device__ __forceinline__ void times(f32x16 (&acc)[N], float f) {
+#pragma unroll
+  for (int t = 0; t < N; ++t) acc[t] *= f;
+}
 __device__ __forceinline__ f32x16 splat16(float x) { return f32x16{x, x, x, x, x, x, x, x, x, x, x, x, x, x, x, x}; }
 
 // the same rows as fp32 partial results, straight from the registers (16 bytes a lane; few of them are written)
@@ -288,6 +314,7 @@ template <typename E, int DP, bool DROP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 32 ? 4 : DP <= 64 ? 3 : 2)))
 void seq_bwd_dq_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
+  constexpr bool SCALED = std::is_same<E, fp16>::value;
   __shared__ __attribute__((aligned(1024))) char lds[4 * I::IMG];
   const int nblk = (a.max_len + 127) / 128, group = a.heads / a.kv_heads;
   const Place at = place(a, group, a.splits_dq);
@@ -330,15 +357,28 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
   }
   D = half_sum(D);
   const bool stats = q < n && lane < 32 && from == 0 && tiles > 0;   // (one of the splits writes them)
+  const float kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
   if (stats) {
     a.nlse2[(long long)h * a.rows + sq.first + q] = nl;
     a.delta[(long long)h * a.rows + sq.first + q] = -D;
   }
+  if constexpr (SCALED) {
+    float norm = 0.f;
+#pragma unroll
+    for (int st = 0; st < DP / 16; ++st) {
+      const typename Vec<E>::x8 x = __builtin_bit_cast(typename Vec<E>::x8, gf[st]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) norm = fmaf(to_f32(x[i]), to_f32(x[i]), norm);
+    }
+    const uint32_t bounds = pack_bounds(kept * __builtin_amdgcn_sqrtf(half_sum(norm)), D);
+    if (stats && lane == 0) a.bounds[(long long)h * a.rows + sq.first + q] = bounds;
+  }
   f32x16 dq[DP / 32];
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t) dq[t] = zero16();
-  const float c = a.scale * LOG2E, kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
-  const float nlc = nl * c;
+  const float c = a.scale * LOG2E;
+  float nlc = nl * c, up = 0.f;
+  if (SCALED) { up = UP_MOST; nlc += up; }
   DropKey key;
   if (DROP) key = drop_key(a.seed, a.site, a.step);
   const auto arrive = [&](int t) {
@@ -374,6 +414,17 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) g[r] *= s[r];
       }
+      if constexpr (SCALED) {
+        const float largest = largest16(g);
+        if (__any(largest > UP_LIMIT)) {
+          const float by = power_down(half_max(largest), up), f = __builtin_amdgcn_exp2f(-by);   // (lanes l and l ^ 32 share a row)
+          up -= by;
+          nlc -= by;
+          s *= f;
+          g *= f;
+          times(dq, f);
+        }
+      }
       // D comes from O as it was stored, off by its rounding: noise in every dS of the row, which is one over the square root of the number of keys of
       // what dS's own rounding does, but all of it where rows see few.  A row of dS has the sum zero (P has the sum 1): where these 32
       // keys are all that the rows see, its sum is D's error, and is taken out.  (Two to four keys: the gradients' error falls from
@@ -384,6 +435,7 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) off += g[r];
           off = half_sum(off);
+          if (SCALED) off *= __builtin_amdgcn_exp2f(-up);
 #pragma unroll
           for (int r = 0; r < 16; ++r) g[r] = fmaf(-s[r], off, g[r]);
           if (stats) a.delta[(long long)h * a.rows + sq.first + q] = -(D + off);
@@ -406,12 +458,13 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
   for (; t < tiles; ++t) arrive(t);
   __syncthreads();
   if (!active) return;
+  const float out_scale = SCALED ? a.scale * __builtin_amdgcn_exp2f(-up) : a.scale;
   if (a.splits_dq > 1) {
     const long long row = (long long)split * a.rows + sq.first + q;
-    store_part<DP>(dq, a.part + row * ((long long)a.heads * a.d) + (long long)h * a.d, q < n, a.d, lane, a.scale);
+    store_part<DP>(dq, a.part + row * ((long long)a.heads * a.d) + (long long)h * a.d, q < n, a.d, lane, out_scale);
     return;
   }
-  store_rows<E, DP>(dq, lds + wave * I::IMG, (E*)a.dq + (sq.first + q0) * a.lddq + (long long)h * a.d, a.lddq, n - q0, a.d, lane, a.scale);
+  store_rows<E, DP>(dq, lds + wave * I::IMG, (E*)a.dq + (sq.first + q0) * a.lddq + (long long)h * a.d, a.lddq, n - q0, a.d, lane, out_scale);
 }
 
 // ---- dK, dV -----------------------------------------------------------------------------------------------------------
@@ -427,6 +480,7 @@ template <typename E, int DP, bool DROP, bool WHOLE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP > 96 ? 1 : 2)))
 void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   using I = Any<DP>;
+  constexpr bool SCALED = std::is_same<E, fp16>::value && !WHOLE;   // (WHOLE: at most 128 keys, and dQ's sums want one power for all of them)
   using IS = Any<64>;                       // dS: [key][64 queries]
   constexpr int STAGE = 2 * I::IMG + 512;   // Q, dO, and 64 rows' -lse and D
   constexpr int KIMG = 2 * STAGE, SIMG = KIMG + 2 * I::IMG, STAT = SIMG + 2 * IS::IMG;   // (WHOLE) K, dS, two heads' -lse and D of 128 rows
@@ -512,6 +566,24 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   const float c = a.scale * LOG2E, kept = DROP ? 256.0f / (256.0f - (float)a.drop) : 1.0f;
   DropKey key;
   if (DROP) key = drop_key(a.seed, a.site, a.step);
+  float up = 0.f;
+  if constexpr (SCALED) {
+    float v_norm = 0.f, norm = 0.f, most_D = 0.f;
+    for (int h = hk * group; h < (hk + 1) * group; ++h)
+      for (int row = lane * 32; row < n; row += 64 * 32) {
+        const uint32_t b2 = a.bounds[(long long)h * a.rows + sq.first + row];
+        norm = fmaxf(norm, __builtin_bit_cast(float, b2 << 16));
+        most_D = fmaxf(most_D, __builtin_bit_cast(float, b2 & 0xFFFF0000u));
+      }
+#pragma unroll
+    for (int st = 0; st < DP / 16; ++st) {
+      const typename Vec<E>::x8 x = __builtin_bit_cast(typename Vec<E>::x8, vf[st]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v_norm = fmaf(to_f32(x[j]), to_f32(x[j]), v_norm);
+    }
+    const float bound = fmaf(wave_max(norm), __builtin_amdgcn_sqrtf(half_sum(v_norm)), wave_max(most_D));
+    up = UP_MOST - power_down(bound * 0x1p14f, UP_MOST);
+  }
   int i = 0;   // tiles so far, of all heads
   const auto arrive = [&] {
     wait_vm0();
@@ -540,7 +612,7 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
         g = mfma_32x32x16<E>(I::rows_frag(Gs, qb * 32 + (lane & 31), st, lane), vf[st], g);
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * c);
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(SCALED ? fmaf(s[r], c, up) : s[r] * c);
       if constexpr (decltype(edge)::value) {
 #pragma unroll
         for (int r = 0; r < 16; ++r)
@@ -651,15 +723,16 @@ void seq_bwd_dkv_kernel(const SeqAttnArgs a) {
   }
   __syncthreads();
   if (!active) return;
+  const float down = SCALED ? __builtin_amdgcn_exp2f(-up) : 1.f, scale_v = kept * down, scale_k = a.scale * down;
   if (a.splits_dkv > 1) {
     const long long width = (long long)a.kv_heads * a.d, row = 2LL * split * a.rows + sq.first + kk;
-    store_part<DP>(dv, a.part + row * width + (long long)hk * a.d, kk < n, a.d, lane, kept);
-    store_part<DP>(dk, a.part + (row + a.rows) * width + (long long)hk * a.d, kk < n, a.d, lane, a.scale);
+    store_part<DP>(dv, a.part + row * width + (long long)hk * a.d, kk < n, a.d, lane, scale_v);
+    store_part<DP>(dk, a.part + (row + a.rows) * width + (long long)hk * a.d, kk < n, a.d, lane, scale_k);
     return;
   }
   char* stage = lds + wave * (STAGE / 2);
-  store_rows<E, DP>(dv, stage, (E*)a.dv + (sq.first + key0) * a.lddv + (long long)hk * a.d, a.lddv, n - key0, a.d, lane, kept);
-  store_rows<E, DP>(dk, stage, (E*)a.dk + (sq.first + key0) * a.lddk + (long long)hk * a.d, a.lddk, n - key0, a.d, lane, a.scale);
+  store_rows<E, DP>(dv, stage, (E*)a.dv + (sq.first + key0) * a.lddv + (long long)hk * a.d, a.lddv, n - key0, a.d, lane, scale_v);
+  store_rows<E, DP>(dk, stage, (E*)a.dk + (sq.first + key0) * a.lddk + (long long)hk * a.d, a.lddk, n - key0, a.d, lane, scale_k);
 }
 
 // ---- partial results of the splits together -------------------------------------------------------------------------------

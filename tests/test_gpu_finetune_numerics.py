@@ -306,3 +306,45 @@ def test_attention_forward_of_scores_far_below_zero(ctx, dtype, n):  # noqa: F81
     assert (np.abs(to_host(x.o[mine]) - ref) <= tol).all()
     score = -(2.0 ** 104) * d * d ** -0.5
     assert (np.abs(to_host(x.lse[0, mine]) - score) <= 4 * E24 * abs(score)).all()
+
+
+@pytest.mark.parametrize("p", [0.0, 0.2])
+@pytest.mark.parametrize("d,causal,size", [(64, False, 1e-3), (64, True, 1e-4), (96, False, 1e-4), (32, True, 1e-3), (128, False, 1e-3), (64, False, 30.0)])
+def test_attention_fp16_gradients_of_any_size(ctx, d, causal, size, p):  # noqa: F811
+    """Long rows spread a gradient over many keys: dS is smaller than dO by the length and may lie below fp16's normal range where its
+    sums over keys or queries do not.  Against fp64, what the results' own rounding leaves and a few half steps of P and dS."""
+    n, heads = 3000, 2
+    x = Problem("fp16", heads, 1, d, [n], causal, p, seed=d)
+    mine = slice(x.first[0], x.first[0] + n)
+    x.do[mine] = (x.do[mine].float() * size).half()
+    x.forward(ctx)
+    x.backward(ctx)
+    ctx.sync()
+    k, v, scale = to_host(x.k[mine]), to_host(x.v[mine]), d ** -0.5
+    dk, dv, parts = 0, 0, []
+    for h in range(heads):
+        c = slice(h * d, h * d + d)
+        Z = F.drop_factors_attention(n, h, p, SEED, SITE)
+        _, _, prob = F.attention(to_host(x.q[mine, c]), k, v, scale, causal, Z)
+        dq, dk1, dv1, _ = F.attention_bwd(to_host(x.q[mine, c]), k, v, scale, Z, prob, to_host(x.do[mine, c]))
+        dk, dv = dk + dk1, dv + dv1
+        parts.append(("dq", to_host(x.dq[mine, c]), dq))
+    for name, got, ref in parts + [("dk", to_host(x.dk[mine]), dk), ("dv", to_host(x.dv[mine]), dv)]:
+        own = np.linalg.norm(ref.astype(np.float16).astype(np.float64) - ref)
+        assert np.linalg.norm(got - ref) <= own + 4 * U["fp16"] * np.linalg.norm(ref), (name, np.linalg.norm(got - ref) / np.linalg.norm(ref), own / np.linalg.norm(ref))
+
+
+@pytest.mark.parametrize("d,causal", [(64, False), (96, True)])
+def test_attention_fp16_gradients_of_rows_of_different_sizes(ctx, d, causal):  # noqa: F811
+    # no gradient at first, then large ones, one of them by far: what the first rows allow must not overflow at the later ones
+    n = 1000
+    x = Problem("fp16", 2, 1, d, [n], causal, 0.0, seed=d, amp=1.5)
+    size = torch.zeros(n, 1, device="cuda")
+    size[400:] = 20.0
+    size[700] = 600.0
+    mine = slice(x.first[0], x.first[0] + n)
+    x.do[mine] = (x.do[mine].float() * size).half()
+    x.forward(ctx)
+    x.backward(ctx)
+    ctx.sync()
+    x.check()
