@@ -342,7 +342,9 @@ int l2l_op_layernorm(l2l_ctx*, int dtype, int rows, int n, const void* x, const 
    rounds (Salmon et al., SC 2011), key = seed, counter words 2 and 3 = site (low, high).  Use another site for
    every place that drops, and another seed or site for every step and micro-batch; a layer recomputed with the same pair sees the same
    mask.  step: device uint64 or NULL; its value when the kernel runs is added to site, so that a captured
-   launch takes another mask when the program has counted it up between replays (forward and backward with the same value). */
+   launch takes another mask when the program has counted it up between replays (forward and backward with the same value).  Sites that share a
+   seed and are used with a step must lie further apart than the steps ever count (multiples of 2^32, say): of neighbouring ones, site s at step
+   t + 1 has the mask of site s + 1 at step t. */
 
 /* Attention over `sequences` sequences in token-major rows.  Sequence b owns the rows first[b] .. first[b] + len[b] - 1 of every
    matrix (device int32 arrays; NULL: first[b] = b max_len, len[b] = max_len), of length 0 to max_len, anywhere in
@@ -373,8 +375,9 @@ int l2l_op_attention(l2l_ctx*, const l2l_attention*, const void* q, long long ld
                      void* o, long long ldo, float* lse, void* work);
 /* Its gradients: dq [rows, heads d], dk, dv [rows, kv_heads d] (summed over the query heads that share them) from dout, the
    gradient of o.  q, k, v, o, lse and the description as in the forward call; the probabilities are computed
-   again, from lse, whose last bit counts: their relative error reaches 2^-21 of the largest |score| (a 16-bit format's half step at scores of some
-   thousands; scores of 2^20 and more leave gradients without a meaning, and from 2^27 on they may be NaN).  No atomics: the same call gives the same bits.  Outputs must not overlap inputs.  work: required. */
+   again, from lse, whose last bit counts: their relative error reaches 2^-21 of the largest |score| (bf16's half step at 8192, fp16's at
+   1024; scores of 2^20 and more leave gradients without a meaning, and from 2^27 on they may be NaN).  No atomics: the same call gives the
+   same bits.  Outputs must not overlap inputs.  work: required. */
 int l2l_op_attention_bwd(l2l_ctx*, const l2l_attention*, const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv,
                          const void* o, long long ldo, const float* lse, const void* dout, long long lddo, void* dq, long long lddq,
                          void* dk, long long lddk, void* dv, long long lddv, void* work);

@@ -169,7 +169,7 @@ def make_config(hidden, heads, ffn, seq, ubatch, num_ubatches, dtype, ln_eps=1e-
 def make_attention(*, dtype, heads, head_dim, sequences, max_len, rows=None, kv_heads=None, first=None, length=None, causal=False,
                    scale=None, dropout=0.0, seed=0, site=0, step=None):
     """Description of an attention call (l2l_attention).  first, length: int32 device tensors or None; step: a one-element int64 device
-    tensor or None; they are kept alive with the description.  Defaults: rows = sequences x max_len, kv_heads = heads, scale = 1 / sqrt(head_dim)."""
+    tensor or None, added to site (sites used with one lie further apart than it counts); they are kept alive with the description.  Defaults: rows = sequences x max_len, kv_heads = heads, scale = 1 / sqrt(head_dim)."""
     a = l2l_attention(DTYPES.get(dtype, dtype), heads, heads if kv_heads is None else kv_heads, head_dim, sequences, max_len,
                       sequences * max_len if rows is None else rows, _ptr(first), _ptr(length), int(bool(causal)),
                       max(1, head_dim) ** -0.5 if scale is None else scale, dropout, _u64(seed), _u64(site), _ptr(step))

@@ -2356,9 +2356,9 @@ static const char* attention_desc_error(const l2l_attention* a) {
 // belong to, so that the launch lasts as long as the longest walk, or as an even share and half a walk more.  Splits shorten the walk, up to
 // four workgroups a compute unit, and cost a launch and their fp32 partial results (`bytes` each).  Measured, whole and chosen splits
 // + their sum (us): one sequence of 2048, 4 query heads on 1 of 64 columns, dropped: forward 40, 19 + 8; dQ 47, 24 + 7; dK and dV
-// 206, 30 + 7.  Two of 1024, 16 heads on 4 of 128: dK and dV 138, 63 + 10; its forward stays whole at 29 (two splits: 31 + 13).  A causal
-// 16384, 32 heads on 8 of 128, stays whole: dK and dV 4520 (two splits: 4445 + 93).  fp32, one causal sequence of
-// 2048, 2 heads on 1 of 128: forward 299, 48 + 16; dQ 401, 59 + 16; dK and dV 1066, 84 + 16.
+// 206, 30 + 7.  Two of 1024, 16 heads on 4 of 128: dK and dV 138, 71 + 12; its forward stays whole at 34 (two splits, when it took 29: 31 + 13).  A causal
+// 16384, 32 heads on 8 of 128, stays whole: dK and dV 4520 (two splits in the same run: 4445 + 93).  fp32, one causal sequence of
+// 2048, 2 heads on 1 of 128: forward 299, 40 + 23; dQ 401, 59 + 16; dK and dV 1066, 84 + 16.
 static int attention_splits(double wgs, int tiles, double total, double us_per_tile, double bytes) {
   int best_s = 1;
   double best = 1e300;

@@ -10,6 +10,11 @@
 // Tiles, fragments and LDS images are those of attention.h: S^T = K Q^T with queries along the lanes in the forward and
 // dQ kernels, S = Q K^T with keys along the lanes in the dK / dV kernel, so that P and dS leave the accumulators as the B
 // operand of the next product.
+//
+// Rounded to E, for the matrix cores: P and dS; everything else between inputs and results is fp32 (scores, maxima, sums, D, accumulators, partial
+// results).  Each rounds once, by half a step at most, and with the result's own rounding a result is 1.4 times as far from 64 bits as that one
+// alone (bf16 0.0023 to 0.0027 of a matrix's norm); P and dS in two halves each would double the products that read them.  D comes from
+// the rounded O, which is seen where rows have few keys (dQ kernel).
 #pragma once
 #include <type_traits>
 
@@ -100,7 +105,8 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[DP / 32], char* s
 // Loads from memory straight into LDS (lane l's 16 or 4 bytes to `dst` + 16 l or 4 l), which have no register to be waited for: the
 // waits are the kernels' own (wait_vm0 at the head of a tile).  As built-ins, the compiler counts them before every transposing LDS read,
 // whose place it does not know, and so takes the next tile's loads for this tile's.  The no-op is the wait state between M0 and
-// its use; nothing else in these kernels uses M0.
+// its use.  M0 is a reserved register, which no clobber list can name: nothing else in these kernels may use it, and in what is compiled from them
+// nothing does.
 __device__ __forceinline__ i32x4 lds_source(const void* base, uint32_t bytes) {
   const uint64_t p = (uint64_t)base;
   return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)p), __builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)) & 0xFFFF,
@@ -186,8 +192,8 @@ __device__ __forceinline__ void store_part(const f32x16 (&acc)[DP / 32], float* 
 // look at the rows' maxima and saves 16 registers: a fourth wave a SIMD at 64 columns also with dropped probabilities.
 // Bound at 64 columns by vector instructions (109 of them, 16 exponentials, to 8 MFMA per wave and 32 keys; 62 % of the SIMDs' clocks at
 // three or more waves), at 128 by the matrix cores.  256 sequences of 128 tokens, 16 heads of 64: 60 us, 4.5 TB/s of the 5.1 that a copy
-// reaches; 64 of up to 512, ragged and dropped: 80 us.  One causal sequence of 16384, 32 heads on 8 of 128: 2200 to 2300 us, 970 TFLOP/s of the visible half
-// (a library product of 8192^3: 1221).
+// reaches; 64 of up to 512, ragged and dropped: 81 us, with vector instructions in 0.55 of the SIMDs' clocks and 2.3 waves a SIMD.  One causal sequence of 16384, 32
+// heads on 8 of 128: 2200 to 2300 us, 970 TFLOP/s of the visible half (a library product of 8192^3: 1221).
 template <typename E, int DP, bool DROP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 64 ? 4 : DP <= 96 && DROP ? 3 : 2)))
 void seq_fwd_kernel(const SeqAttnArgs a) {
@@ -309,7 +315,8 @@ void seq_fwd_kernel(const SeqAttnArgs a) {
 
 // ---- dQ, and what the dK / dV kernel needs of each row ----------------------------------------------------------------
 // As the forward kernel, with dP beside S and dS K in the place of P V.  Bound by vector instructions and the latency of its three dependent
-// products at 64 columns (64 sequences of up to 512, 16 heads, dropped: 98 us; at two waves a SIMD a tenth more), by the matrix cores at 128 (one causal sequence of 16384, 32 heads on 8: 2950 us, 1120 TFLOP/s).
+// products at 64 columns (64 sequences of up to 512, 16 heads, dropped: 97 to 101 us; at two waves a SIMD a tenth more), by
+// the matrix cores at 128 (one causal sequence of 16384, 32 heads on 8: 2850 to 2990 us, 1100 to 1160 TFLOP/s).
 template <typename E, int DP, bool DROP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP <= 32 ? 4 : DP <= 64 ? 3 : 2)))
 void seq_bwd_dq_kernel(const SeqAttnArgs a) {
@@ -471,11 +478,12 @@ void seq_bwd_dq_kernel(const SeqAttnArgs a) {
 // A workgroup owns 128 keys of one (sequence, key head) and walks the queries of all the head's query heads in tiles of 64.
 // WHOLE, where no sequence is longer than 128: the workgroup has all keys of its head, so that dQ of a tile can be made here as well, from dS
 // that the waves lay side by side in LDS, and the dQ kernel with its second pass over scores, probabilities and masks is not run.  The
-// rows' D and lse are taken from O, dO and lse at the head's start.  (256 sequences of up to 128, 16 heads of 64, dropped: 119 us, the two
-// kernels 143; wider heads leave no registers for it.)
-// Bound at 64 columns by latency at two waves a SIMD (235 to 256 registers; at three they spill): 64 ragged sequences of up to 512, dropped,
-// 121 us; WHOLE by its first loads, half of a workgroup's life (256 of 128 tokens: 143 us, 3.7 TB/s), at 128 columns, one wave a SIMD,
-// by the matrix cores (one causal sequence of 16384, 32 heads on 8: 4600 us, 955 TFLOP/s).
+// rows' D and lse are taken from O, dO and lse at the head's start.  (256 sequences of up to 128, 16 heads of 64, dropped: 119 to 122 us, the
+// two kernels 143; wider heads leave no registers for it.)
+// Bound at 64 columns by latency at two waves a SIMD (226 and 240 registers; at three they spill): 64 ragged sequences of up to 512, dropped, 115 to
+// 121 us; WHOLE by its first loads, half of a workgroup's life (256 of 128 tokens: 148 us, 3.6 TB/s).  WHOLE takes 245 registers; dropped it takes
+// all 256 and spills 14 vector and 67 scalar ones (at 32 columns 192, and 62 scalar ones).  At 128 columns one wave a SIMD (292 registers, dropped
+// 314), bound by the matrix cores and what that wave waits for (one causal sequence of 16384, 32 heads on 8: 4830 to 5220 us, 840 to 910 TFLOP/s).
 template <typename E, int DP, bool DROP, bool WHOLE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DP > 96 ? 1 : 2)))
 void seq_bwd_dkv_kernel(const SeqAttnArgs a) {

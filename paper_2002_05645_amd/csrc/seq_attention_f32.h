@@ -7,7 +7,7 @@
 // PARTS = 2, where the longest sequence has 33 to 64 rows: the waves that have no rows of the workgroup's 128 take every other tile of the
 // others' rows, and the two results are put together in LDS.  4 sequences of 64, 2 heads of 64, dropped: forward 9.0 -> 7.1 us,
 // dQ 12.3 -> 11.1, dK and dV 13.3 -> 10.6; 256 ragged ones, 12 heads: 56 -> 56, 89 -> 82, 103 -> 83.  (Of 32 or fewer rows there is one
-// tile, and the second buffers only cost: 34 -> 45, 54 -> 63, 62 -> 68.)
+// tile, and the second buffers only cost: 34 -> 45, 54 -> 63, 62 -> 68.)  Its dK / dV kernel at 64 columns takes 257 registers, dropped 262: one wave a SIMD.
 #pragma once
 #include "seq_attention.h"
 
