@@ -348,3 +348,49 @@ def test_attention_fp16_gradients_of_rows_of_different_sizes(ctx, d, causal):  #
     x.backward(ctx)
     ctx.sync()
     x.check()
+
+
+def test_attention_fp16_backward_gives_the_same_bits_captured_and_in_any_workspace():
+    # what the dQ kernel leaves for the dK / dV kernel is written anew by every call
+    stream = torch.cuda.Stream()
+    c = P.Context(P.make_config(64, 2, 128, 16, 2, 2, "bf16", 1e-5, 0), stream.cuda_stream, stream.cuda_stream)
+    try:
+        for lengths in ([300, 257, 64, 1], [1500]):
+            x = Problem("fp16", 4, 2, 64, lengths, True, 0.1, seed=6)
+            outs = (x.o, x.lse, x.dq, x.dk, x.dv)
+
+            def both():
+                x.forward(c)
+                x.backward(c)
+            torch.cuda.synchronize()
+            both()
+            torch.cuda.synchronize()
+            eager = [t.clone() for t in outs]
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                both()
+            for fill in (255, 0, 127):
+                for t in outs:
+                    t.fill_(7.0)
+                x.work.fill_(fill)
+                torch.cuda.synchronize()
+                with torch.cuda.stream(stream):
+                    graph.replay()
+                torch.cuda.synchronize()
+                torch.randn(1000, device="cuda").sum().item()
+                assert all(torch.equal(a, b) for a, b in zip(outs, eager))
+            x.check()
+    finally:
+        c.close()
+
+
+def test_attention_in_parts_without_lse(ctx):  # noqa: F811
+    for dtype in ("bf16", "fp32"):
+        x = Problem(dtype, 2, 1, 64, [1100, 300], False, 0.0, seed=12)
+        x.forward(ctx)
+        ctx.sync()
+        o = x.o.clone()
+        x.o.fill_(7.0)
+        ctx.op_attention(x.plan, x.q, x.q.stride(0), x.k, x.k.stride(0), x.v, x.v.stride(0), x.o, x.o.stride(0), None, x.work)
+        ctx.sync()
+        assert torch.equal(x.o, o)
